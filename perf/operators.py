@@ -375,7 +375,7 @@ def _append8(x, case, kv, new):
     scales[at] = (e + 127).to(torch.uint8)
     whole = torch.zeros((pool.shape[0], hkv), dtype=torch.int32, device=new.device)
     whole[at] = e
-    codes = (new * _power(-whole[block])[..., None]).clamp(-448, 448).to(torch.float8_e4m3fn)
+    codes = (new * _power(-whole[block])[..., None]).to(torch.float8_e4m3fn)   # at most 448 by the choice of e
     pool[block, row] = codes.view(torch.uint8)
 
 
@@ -513,7 +513,6 @@ def _exact_turn(rows, case, x):
 
 def _exact_code(y):
     """Nearest e4m3 value: steps of 2^-9 below 2^-6, else an eighth of the power of two below."""
-    y = y.clamp(-448, 448)
     step = torch.exp2(torch.floor(torch.log2(y.abs().clamp(min=2.0 ** -6))) - 3)
     return torch.round(y / step) * step
 
