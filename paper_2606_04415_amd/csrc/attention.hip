@@ -56,6 +56,7 @@ __device__ __forceinline__ void merge_rows(const AttnParams& p, const int32_t* i
   const int64_t out_row0 = int64_t(it[6]) * p.Hq + int64_t(col) * rows;
   for (int idx = blockIdx.z * blockDim.x + threadIdx.x; idx < rows * (DV / 4); idx += blockDim.x * gridDim.z) {
     const int i = idx / (DV / 4);
+    if (col * rows + i >= p.Hq) break;   // the last column may cover fewer heads; later rows lie past it too
     const int d = 4 * (idx % (DV / 4));
     float M = -INFINITY, den = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
