@@ -35,8 +35,9 @@
  *  - Run calls (decode, prefill, mixed, debug gather, workspace init) only
  *    enqueue work on the given HIP stream (a hipStream_t passed as void*;
  *    NULL is the null stream) and return; they never synchronise.
- *  - Tensors are bf16 with the innermost dimension contiguous; every base
- *    pointer and every row stride must be a multiple of 16 bytes.
+ *  - Tensors are bf16 (8-bit caches: e4m3) with the innermost dimension
+ *    contiguous; every base pointer and every row stride must be a multiple
+ *    of 16 bytes.
  */
 #ifndef FLEXATTN_H
 #define FLEXATTN_H
@@ -116,6 +117,10 @@ typedef struct flex_attn_plan_opts {
                                  two groups of ranges, the second (the tail) run on the
                                  prefill stream after the prefill (see flex_attn_mixed);
                                  -1: no tail [0] */
+  int32_t kv_bits;            /* bits of a cached value: 16 (bf16), or 8 for the calls over an 8-bit
+                                 cache (flex_attn_decode_kv8 and its like; grouped-query heads
+                                 only, bm 128 only, no one-launch form). A plan serves the calls
+                                 of its own cache type only [16] */
 } flex_attn_plan_opts;
 
 /* Summary of a plan. */
@@ -408,6 +413,150 @@ typedef struct flex_attn_append_args {
 } flex_attn_append_args;
 
 int flex_attn_kv_append(const flex_attn_shape* shape, const flex_attn_append_args* args, void* stream);
+
+/* Rotary positions: how the appends below turn queries and keys. In the
+ * rot_dim columns from rot_begin of every head, pair i (0 <= i < rot_dim / 2)
+ * of values (x, y) becomes (x c - y s, y c + x s), in fp32 with one rounding at
+ * the end, c and s read from the table at the token's position on the pair's
+ * axis. The other columns pass unchanged.
+ *  cos_sin      fp32 [max_position][rot_dim], device, contiguous: the cosines
+ *               of the rot_dim / 2 pairs, then their sines.
+ *  positions    int32 [n_axes][n_tokens], device; axis a's row starts at
+ *               element a * positions_stride. flex_attn_kv8_append takes NULL
+ *               with one axis: token i of n new ones is at L - n + i. A token
+ *               with a position outside [0, max_position) is skipped: nothing
+ *               of it is written, and *bad_count grows by 1.
+ *  rot_begin, rot_dim   multiples of 8 and 16; rot_begin + rot_dim <= d_qk.
+ *  neighbours   0: pair i is columns (i, i + rot_dim / 2) of the part; 1:
+ *               columns (2 i, 2 i + 1).
+ *  n_axes       1 to 4 (time, height, width, ...). With more than one, axis a
+ *               has sections[a] >= 0 pairs, which sum to rot_dim / 2.
+ *  dealt        0: the sections follow each other (the first sections[0] pairs
+ *               go by axis 0, the next by axis 1, ...); 1: pairs are dealt out
+ *               in turn, pair i to axis a = i % n_axes while axis a has pairs
+ *               left (i < n_axes * sections[a]), otherwise to axis 0. */
+#define FLEX_ROPE_MAX_AXES 4
+typedef struct flex_attn_rope {
+  const float* cos_sin;
+  const int32_t* positions;
+  int64_t positions_stride;
+  int32_t max_position;
+  int32_t rot_begin;
+  int32_t rot_dim;
+  int32_t neighbours;
+  int32_t n_axes;
+  int32_t dealt;
+  int32_t sections[FLEX_ROPE_MAX_AXES];
+} flex_attn_rope;
+
+/* KV append with the position rotation applied on the way, for every supported
+ * shape: a step's queries and keys are read once as the projections left them,
+ * turned, and written where the attention reads them.
+ *  kv       as for flex_attn_kv_append (its slot rules included); keys are
+ *           turned, values copied. A token that its slot or its positions skip
+ *           has no query written either; one at fault on both counts is
+ *           counted once.
+ *  q        bf16 [n_tokens][Hq][d_qk]: token t's row starts at element
+ *           t * q_stride; the Hq*d_qk values of a row are contiguous.
+ *  q_out    bf16 [n_tokens][Hq][d_qk], contiguous. May be q itself when
+ *           q_stride is Hq*d_qk; otherwise they must not overlap.
+ * Enqueues one kernel on stream and returns. */
+typedef struct flex_attn_rope_append_args {
+  flex_attn_append_args kv;
+  const void* q;
+  int64_t q_stride;
+  void* q_out;
+} flex_attn_rope_append_args;
+
+int flex_attn_rope_append(const flex_attn_shape* shape, const flex_attn_rope* rope,
+                          const flex_attn_rope_append_args* args, void* stream);
+
+/* ------------------------------------------------------------------------
+ * 8-bit caches (grouped-query heads of 64 or 128).
+ *
+ * k_cache and v_cache hold e4m3 codes (OCP, 0x7F and 0xFF are NaN) in the
+ * bf16 caches' layout, strides in bytes. Each block of 16 tokens of a page
+ * has, for each KV head, one scale for its keys and one for its values: a byte
+ * b that stands for 2^(b - 127) (e8m0; 255 is NaN, 0 is taken as 0). A cached
+ * value is code * scale. Scales are powers of two because the matrix-core
+ * operands are bf16: a scaled code is then a bf16 value exactly, so attention
+ * over the cache loses nothing beyond the one rounding of the append.
+ *  kv_scales  bytes [num_pages][page_size / 16][Hkv][2] (key, value): page p
+ *             starts at byte p * scale_page_stride, the rest is contiguous;
+ *             base and stride are multiples of 2 bytes.
+ * ---------------------------------------------------------------------- */
+
+/* KV append into an 8-bit cache, turning queries and keys on the way when rope
+ * is given (NULL: keys are stored as they are and q is ignored).
+ *
+ * The new tokens are the batch's, as the attention calls take it: sequence s
+ * has tokens query_start_loc[s] .. query_start_loc[s + 1] - 1 of the new rows
+ * and holds seq_lens[s] tokens after the call, in the pages of its
+ * block_table row. Rows of k_new, v_new, q and q_out past
+ * query_start_loc[num_seqs] (padding) are neither read nor written.
+ *
+ * Per block with new rows, KV head and K / V: with a the largest magnitude
+ * among the new rows' finite values, the scale is the least 2^k, k >= -117,
+ * with a <= 448 * 2^k, but not below the scale that the block has, if it holds
+ * earlier rows of the sequence (its first new row is not row 0). Where a scale
+ * grows, the earlier rows' codes are rewritten for it (their values stay,
+ * except below 2^-6 of the new scale, where they round again). New codes are
+ * value / scale rounded to nearest even; values that are not finite become NaN.
+ *
+ * A token is skipped, and *bad_count grows by 1, when its page index is
+ * beyond block_table_stride, its page outside [0, num_pages), or one of its
+ * positions outside [0, max_position); a skipped token's row within a block
+ * that other tokens write is unspecified. Two sequences must not append to
+ * one block in the same call.
+ *  k_new, v_new, strides, n_tokens, num_pages, bad_count: as in
+ *             flex_attn_append_args; n_tokens >= query_start_loc[num_seqs]
+ *             (tokens past n_tokens are not appended).
+ *  q, q_stride, q_out   as in flex_attn_rope_append_args.
+ * Enqueues one kernel on stream and returns. */
+typedef struct flex_attn_kv8_append_args {
+  const void* k_new;
+  const void* v_new;
+  int64_t k_new_stride;
+  int64_t v_new_stride;
+  const void* q;
+  int64_t q_stride;
+  void* q_out;
+  int64_t n_tokens;
+  int32_t num_seqs;
+  const int32_t* block_table;
+  int32_t block_table_stride;
+  const int32_t* seq_lens;
+  const int32_t* query_start_loc;
+  void* k_cache;
+  int64_t k_stride[3];
+  void* v_cache;
+  int64_t v_stride[3];
+  void* kv_scales;
+  int64_t scale_page_stride;
+  int64_t num_pages;
+  int32_t* bad_count;
+} flex_attn_kv8_append_args;
+
+int flex_attn_kv8_append(const flex_attn_shape* shape, const flex_attn_rope* rope,
+                         const flex_attn_kv8_append_args* args, void* stream);
+
+/* Attention over an 8-bit cache: flex_attn_decode, _prefill and _mixed with
+ * cached values code * scale, on a plan made with kv_bits = 8. attn's caches
+ * and strides are those of the 8-bit cache (strides in bytes); everything else
+ * in it, outputs, workspace and debug mode included, is as for those calls.
+ * FLEX_MODE_FUSED is FLEX_ERR_UNSUPPORTED. A NaN in a value row reaches the
+ * queries that attend it and may reach others of the same tile of 32 keys of
+ * that sequence; slots past a sequence's end never count. */
+typedef struct flex_attn_kv8_args {
+  flex_attn_args attn;
+  const void* kv_scales;
+  int64_t scale_page_stride;
+} flex_attn_kv8_args;
+
+int flex_attn_decode_kv8(const flex_attn_plan_t* plan, const flex_attn_kv8_args* args, void* stream);
+int flex_attn_prefill_kv8(const flex_attn_plan_t* plan, const flex_attn_kv8_args* args, void* stream);
+int flex_attn_mixed_kv8(const flex_attn_plan_t* plan, const flex_attn_kv8_args* args, int mode, void* stream,
+                        flex_attn_corun_t* corun);
 
 /* ------------------------------------------------------------------------
  * Online co-location controller (host only, no HIP call).

@@ -46,6 +46,9 @@ the contract is:
   grouped-query default is 128 when F = sum over prefill sequences of
   ceil(n * G / 128) * Hkv satisfies F >= 4 * cus_prefill, or
   F <= 3 * cus_prefill with cus_prefill < cus_total (a co-run share), else 32.
+  Plans for 8-bit caches (kv_bits 8, grouped-query heads only) always take 128;
+  their decode bytes count one byte a value and two scale bytes for each 16
+  tokens and KV head.
 * co-run CU split: explicit, or (cus_decode = -1) the argmin over multiples of
   the granule of the step time, smallest n_d on ties: with t_p =
   prefill_flops / ((cus_total - n_d) * flops_cu) and r_s = min(hbm, n_d *
@@ -125,6 +128,7 @@ class Opts:
     decode_gbps_per_cu: float = 0.0   # 0 -> 43
     prefill_tflops_per_cu: float = 0.0  # 0 -> 4
     decode_tail: int = 0         # 0 -> a tail group of ranges on grouped-query co-run plans; -1 -> none
+    kv_bits: int = 0             # 0 or 16 -> bf16 caches; 8 -> 8-bit caches (grouped-query heads, BM 128)
 
 
 @dataclass
@@ -179,6 +183,12 @@ def build_plan(sh: Shape, opts: Optional[Opts], qsl: Sequence[int], seq_lens: Se
         return PlanResult(ERR_INVALID_ARG)
     if o.decode_tail not in (0, -1):
         return PlanResult(ERR_INVALID_ARG)
+    if o.kv_bits not in (0, 8, 16):
+        return PlanResult(ERR_INVALID_ARG)
+    if o.kv_bits == 8:
+        if mla or split or bm not in (0, 128):
+            return PlanResult(ERR_UNSUPPORTED)
+        bm = 128
     if o.cus_decode < -1 or o.cus_decode > cus_total:
         return PlanResult(ERR_INVALID_ARG)
     if (mla and bm not in (64, 128)) or (split and bm != 128) or (
@@ -209,7 +219,10 @@ def build_plan(sh: Shape, opts: Optional[Opts], qsl: Sequence[int], seq_lens: Se
     dec_bytes = 0
     kv_row = sh.num_kv_heads * (sh.head_dim_qk if sh.v_aliases_k else sh.head_dim_qk + sh.head_dim_v) * 2
     for s in dec:
-        dec_bytes += seq_lens[s] * kv_row
+        if o.kv_bits == 8:   # a byte a value, and two scale bytes for each 16 tokens and head
+            dec_bytes += seq_lens[s] * (kv_row // 2) + cdiv(seq_lens[s], 16) * sh.num_kv_heads * 2
+        else:
+            dec_bytes += seq_lens[s] * kv_row
     pre_flops = 0
     for s in pre:
         n, L = qsl[s + 1] - qsl[s], seq_lens[s]

@@ -18,6 +18,8 @@ CSRC = os.path.join(PKG, "csrc")
 ROOT = os.path.dirname(PKG)
 LIB = os.path.join(PKG, "libflexattn.so")
 SOURCES = ["attention.hip", "latent.hip", "kv_append.hip", "api.hip", "plan.cpp", "controller.cpp"]
+# sources whose values may be NaN: what they copy or quantise is the caller's
+KEEPS_NANS = {"kv_append.hip"}
 ARCH = "gfx950"
 
 
@@ -28,14 +30,16 @@ def hipcc() -> str:
     raise RuntimeError("hipcc not found (ROCm is required to build libflexattn.so)")
 
 
-def common_flags():
-    return ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",
-            # keep the compiler from forming packed fp32 VALU instructions
-            "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-            # scores are finite; max() needs no NaN quieting (a NaN from a wrong
-            # page still reaches the output through the P x V product)
-            "-fno-honor-nans",
-            "-I", os.path.join(ROOT, "include"), "-Wall", "-Wno-unused-function"]
+def common_flags(src: str = ""):
+    flags = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",
+             # keep the compiler from forming packed fp32 VALU instructions
+             "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
+             "-I", os.path.join(ROOT, "include"), "-Wall", "-Wno-unused-function"]
+    if src not in KEEPS_NANS:
+        # scores are finite; max() needs no NaN quieting (a NaN from a wrong
+        # page still reaches the output through the P x V product)
+        flags.append("-fno-honor-nans")
+    return flags
 
 
 def build(verbose: bool = False) -> str:
@@ -45,7 +49,7 @@ def build(verbose: bool = False) -> str:
 
     def compile_one(src):
         obj = os.path.join(bdir, os.path.splitext(src)[0] + ".o")
-        cmd = [cc] + common_flags() + ["-c", os.path.join(CSRC, src), "-o", obj]
+        cmd = [cc] + common_flags(src) + ["-c", os.path.join(CSRC, src), "-o", obj]
         if src.endswith(".cpp"):
             cmd = [cc, "-x", "hip"] + cmd[1:]
         r = subprocess.run(cmd, capture_output=True, text=True)

@@ -53,11 +53,30 @@ int hip_fail(hipError_t e, const char* what) {
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
+int check_kv_bits(const flex_attn_plan_t* plan, int bits) {
+  if (plan->kv_bits == bits) return FLEX_OK;
+  return set_error(FLEX_ERR_INVALID_ARG, "the plan is for " + std::to_string(plan->kv_bits) + "-bit caches (kv_bits)");
+}
+
+// Scales of an 8-bit cache: bytes [page][page_size / 16][Hkv][2].
+int check_scales(const flex_attn_shape& sh, const void* scales, int64_t page_stride) {
+  if (!scales || (reinterpret_cast<uintptr_t>(scales) & 1u))
+    return set_error(FLEX_ERR_INVALID_ARG, "kv_scales must be non-NULL and 2-byte aligned");
+  if (page_stride < int64_t(sh.page_size) / kKv8Block * sh.num_kv_heads * 2 || page_stride % 2 ||
+      page_stride >= int64_t(1) << 31)
+    return set_error(FLEX_ERR_INVALID_ARG, "scale_page_stride must be even, below 2^31 and cover page_size / 16 * Hkv * 2 bytes");
+  return FLEX_OK;
+}
+
 // Checks shared by every run call; fills the kernel parameter block. A
 // non-NULL ws_override (of at least the plan's workspace_bytes) replaces the
-// caller's workspace, whose fields are then ignored.
-int prepare(const flex_attn_plan_t* plan, const flex_attn_args* a, AttnParams* p, void* ws_override = nullptr) {
+// caller's workspace, whose fields are then ignored. kv8: the call's arguments
+// when it is one over an 8-bit cache (a is their attn).
+int prepare(const flex_attn_plan_t* plan, const flex_attn_args* a, AttnParams* p, void* ws_override = nullptr,
+            const flex_attn_kv8_args* kv8 = nullptr) {
   if (!plan || !a) return set_error(FLEX_ERR_INVALID_ARG, "plan or args is NULL");
+  if (const int st = check_kv_bits(plan, kv8 ? 8 : 16); st != FLEX_OK) return st;
+  const int64_t esz = kv8 ? 1 : 2;   // bytes of a cached value
   const flex_attn_shape& sh = plan->shape;
   const flex_attn_plan_info& info = plan->info;
   const bool has_work = info.n_decode_items + info.n_prefill_items > 0;
@@ -71,14 +90,16 @@ int prepare(const flex_attn_plan_t* plan, const flex_attn_args* a, AttnParams* p
     return set_error(FLEX_ERR_INVALID_ARG, "q, caches, out and d_plan must be 16-byte aligned");
   const int64_t* vs = sh.v_aliases_k ? a->k_stride : a->v_stride;
   for (int i = 0; i < 3; ++i) {
-    if (a->k_stride[i] <= 0 || vs[i] <= 0 || (a->k_stride[i] * 2) % 16 || (vs[i] * 2) % 16)
+    if (a->k_stride[i] <= 0 || vs[i] <= 0 || (a->k_stride[i] * esz) % 16 || (vs[i] * esz) % 16)
       return set_error(FLEX_ERR_INVALID_ARG, "cache strides must be positive multiples of 16 bytes");
   }
   // Within a page the kernels use 32-bit byte offsets.
   const int64_t lim = int64_t(1) << 31;
-  if (a->k_stride[0] * 2 >= lim || vs[0] * 2 >= lim || a->k_stride[1] * 2 * sh.page_size >= lim ||
-      vs[1] * 2 * sh.page_size >= lim)
+  if (a->k_stride[0] * esz >= lim || vs[0] * esz >= lim || a->k_stride[1] * esz * sh.page_size >= lim ||
+      vs[1] * esz * sh.page_size >= lim)
     return set_error(FLEX_ERR_INVALID_ARG, "cache page stride or page_size * slot stride reaches 2^31 bytes");
+  if (kv8)
+    if (const int st = check_scales(sh, kv8->kv_scales, kv8->scale_page_stride); st != FLEX_OK) return st;
   if (a->k_stride[2] < sh.head_dim_qk || vs[2] < (sh.v_aliases_k ? sh.head_dim_qk : sh.head_dim_v))
     return set_error(FLEX_ERR_INVALID_ARG, "cache head stride smaller than the head dimension");
   if (a->num_pages <= 0) return set_error(FLEX_ERR_INVALID_ARG, "num_pages must be positive");
@@ -109,6 +130,10 @@ int prepare(const flex_attn_plan_t* plan, const flex_attn_args* a, AttnParams* p
   p->P = sh.page_size;
   p->rows_per_wg = plan->rows_per_wg;
   p->scale_log2 = sh.sm_scale * 1.4426950408889634f;
+  if (kv8) {
+    p->kv_scales = static_cast<const uint8_t*>(kv8->kv_scales);
+    p->scale_sp = kv8->scale_page_stride;
+  }
   if (info.workspace_bytes > 0) {
     const int32_t W = info.decode_wg_width;
     const size_t stats = size_t(info.n_decode_items) * W * plan->rows_per_wg * 2 * 4;
@@ -343,12 +368,13 @@ bool long_step(const flex_attn_plan_t* plan, const flex_attn_corun* c) {
 }
 
 int run_mixed(const flex_attn_plan_t* plan, const flex_attn_args* args, int mode, void* stream,
-              flex_attn_corun_t* corun, void* ws_override) {
+              flex_attn_corun_t* corun, void* ws_override, const flex_attn_kv8_args* kv8 = nullptr) {
   if (mode != FLEX_MODE_SERIAL && mode != FLEX_MODE_CORUN && mode != FLEX_MODE_FUSED)
     return set_error(FLEX_ERR_INVALID_ARG, "unknown mode");
   AttnParams p;
-  int st = prepare(plan, args, &p, ws_override);
+  int st = prepare(plan, args, &p, ws_override, kv8);
   if (st != FLEX_OK) return st;
+  if (kv8 && mode == FLEX_MODE_FUSED) return set_error(FLEX_ERR_UNSUPPORTED, "no one-launch form over an 8-bit cache");
   hipStream_t s = static_cast<hipStream_t>(stream);
   if ((st = debug_validate(plan, args, s)) != FLEX_OK) return st;
   if (mode == FLEX_MODE_FUSED) return run_fused(plan, p, args, s);
@@ -453,10 +479,38 @@ extern "C" int flex_attn_mixed(const flex_attn_plan_t* plan, const flex_attn_arg
   return run_mixed(plan, args, mode, stream, corun, nullptr);
 }
 
+extern "C" int flex_attn_decode_kv8(const flex_attn_plan_t* plan, const flex_attn_kv8_args* args, void* stream) {
+  clear_error();
+  if (!args) return set_error(FLEX_ERR_INVALID_ARG, "plan or args is NULL");
+  AttnParams p;
+  int st = prepare(plan, &args->attn, &p, nullptr, args);
+  if (st != FLEX_OK) return st;
+  if ((st = debug_validate(plan, &args->attn, static_cast<hipStream_t>(stream))) != FLEX_OK) return st;
+  return run_decode(plan, p, &args->attn, static_cast<hipStream_t>(stream));
+}
+
+extern "C" int flex_attn_prefill_kv8(const flex_attn_plan_t* plan, const flex_attn_kv8_args* args, void* stream) {
+  clear_error();
+  if (!args) return set_error(FLEX_ERR_INVALID_ARG, "plan or args is NULL");
+  AttnParams p;
+  int st = prepare(plan, &args->attn, &p, nullptr, args);
+  if (st != FLEX_OK) return st;
+  if ((st = debug_validate(plan, &args->attn, static_cast<hipStream_t>(stream))) != FLEX_OK) return st;
+  return run_prefill(plan, p, &args->attn, static_cast<hipStream_t>(stream));
+}
+
+extern "C" int flex_attn_mixed_kv8(const flex_attn_plan_t* plan, const flex_attn_kv8_args* args, int mode,
+                                   void* stream, flex_attn_corun_t* corun) {
+  clear_error();
+  if (!args) return set_error(FLEX_ERR_INVALID_ARG, "plan or args is NULL");
+  return run_mixed(plan, &args->attn, mode, stream, corun, nullptr, args);
+}
+
 extern "C" int flex_attn_mixed_static(const flex_attn_plan_t* plan, const flex_attn_args* args, int mode,
                                       void* stream, flex_attn_corun_t* corun) {
   clear_error();
   if (!plan || !args) return set_error(FLEX_ERR_INVALID_ARG, "plan or args is NULL");
+  if (const int st = check_kv_bits(plan, 16); st != FLEX_OK) return st;
   if (plan->info.workspace_bytes > kStaticScratchBytes)
     return set_error(FLEX_ERR_WORKSPACE, "the plan needs " + std::to_string(plan->info.workspace_bytes) +
                                              " bytes of split-K scratch; the allocation-free call holds " +
@@ -593,6 +647,7 @@ extern "C" int flex_attn_debug_gather(const flex_attn_plan_t* plan, const flex_a
   if (!plan || !a || !a->k_cache || !a->block_table || !k_out)
     return set_error(FLEX_ERR_INVALID_ARG, "NULL argument");
   const flex_attn_shape& sh = plan->shape;
+  if (plan->kv_bits != 16) return set_error(FLEX_ERR_UNSUPPORTED, "no debug gather over an 8-bit cache");
   if (seq < 0 || seq >= plan->info.num_seqs) return set_error(FLEX_ERR_INVALID_ARG, "seq out of range");
   if (seq_len < 0) return set_error(FLEX_ERR_INVALID_ARG, "seq_len < 0");
   const bool has_v = !sh.v_aliases_k;
@@ -616,12 +671,10 @@ extern "C" int flex_attn_workspace_init(void* workspace, size_t bytes, void* str
   return e == hipSuccess ? FLEX_OK : hip_fail(e, "fill launch");
 }
 
-extern "C" int flex_attn_kv_append(const flex_attn_shape* shape, const flex_attn_append_args* a, void* stream) {
-  clear_error();
-  if (!shape || !a) return set_error(FLEX_ERR_INVALID_ARG, "shape or args is NULL");
-  if (const int st = check_shape(*shape); st != FLEX_OK) return st;
-  if (a->n_tokens < 0) return set_error(FLEX_ERR_INVALID_ARG, "n_tokens < 0");
-  if (a->n_tokens == 0) return FLEX_OK;
+namespace {
+
+// Checks of an append of n_tokens > 0 tokens; fills the kernel parameter block.
+int prepare_append(const flex_attn_shape* shape, const flex_attn_append_args* a, AppendParams* out) {
   const bool has_v = !shape->v_aliases_k;
   if (!a->k_new || !a->slot_mapping || !a->k_cache || (has_v && (!a->v_new || !a->v_cache)))
     return set_error(FLEX_ERR_INVALID_ARG, "a required pointer is NULL");
@@ -638,7 +691,8 @@ extern "C" int flex_attn_kv_append(const flex_attn_shape* shape, const flex_attn
   if (a->k_stride[2] < dk || (has_v && a->v_stride[2] < dv))
     return set_error(FLEX_ERR_INVALID_ARG, "cache head stride smaller than the head dimension");
   if (a->num_pages <= 0) return set_error(FLEX_ERR_INVALID_ARG, "num_pages must be positive");
-  AppendParams p{};
+  AppendParams& p = *out;
+  p = AppendParams{};
   p.k_new = static_cast<const uint16_t*>(a->k_new);
   p.v_new = static_cast<const uint16_t*>(has_v ? a->v_new : a->k_new);
   p.k_new_stride = a->k_new_stride;
@@ -655,6 +709,160 @@ extern "C" int flex_attn_kv_append(const flex_attn_shape* shape, const flex_attn
   p.ck = Hkv * dk / 8;
   p.cv = has_v ? Hkv * dv / 8 : 0;
   p.bad_count = a->bad_count;
+  return FLEX_OK;
+}
+
+// Checks of a rotation of n_tokens > 0 tokens; fills the kernel parameter block.
+int prepare_rope(const flex_attn_shape& sh, const flex_attn_rope* r, int64_t n_tokens, bool own_positions,
+                 RopeParams* p) {
+  if (!r->cos_sin || !aligned16(r->cos_sin))
+    return set_error(FLEX_ERR_INVALID_ARG, "cos_sin must be non-NULL and 16-byte aligned");
+  if (r->max_position <= 0) return set_error(FLEX_ERR_INVALID_ARG, "max_position must be positive");
+  if (r->rot_dim <= 0 || r->rot_dim % 16 || r->rot_begin < 0 || r->rot_begin % 8 ||
+      int64_t(r->rot_begin) + r->rot_dim > sh.head_dim_qk)
+    return set_error(FLEX_ERR_INVALID_ARG, "rot_dim must be a positive multiple of 16, rot_begin one of 8, within the head");
+  if (r->n_axes < 1 || r->n_axes > FLEX_ROPE_MAX_AXES)
+    return set_error(FLEX_ERR_INVALID_ARG, "n_axes must be 1 to 4");
+  if ((r->neighbours != 0 && r->neighbours != 1) || (r->dealt != 0 && r->dealt != 1))
+    return set_error(FLEX_ERR_INVALID_ARG, "neighbours and dealt must be 0 or 1");
+  if (!r->positions && (!own_positions || r->n_axes > 1)) return set_error(FLEX_ERR_INVALID_ARG, "positions is NULL");
+  const int32_t pairs = r->rot_dim / 2;
+  if (r->n_axes > 1) {
+    if (r->positions_stride < n_tokens)
+      return set_error(FLEX_ERR_INVALID_ARG, "positions_stride is below n_tokens");
+    int64_t sum = 0;
+    for (int a = 0; a < r->n_axes; ++a) {
+      const int64_t n = r->sections[a];
+      if (n < 0 || n > pairs) return set_error(FLEX_ERR_INVALID_ARG, "a section is negative or exceeds the pairs");
+      if (r->dealt && a > 0 && n > 0 && a + (n - 1) * r->n_axes >= pairs)
+        return set_error(FLEX_ERR_INVALID_ARG, "a section is longer than the pairs its axis is dealt");
+      sum += n;
+    }
+    if (sum != pairs) return set_error(FLEX_ERR_INVALID_ARG, "sections must sum to rot_dim / 2");
+  }
+  *p = RopeParams{};
+  p->cos_sin = r->cos_sin;
+  p->positions = r->positions;
+  p->positions_stride = r->n_axes > 1 ? r->positions_stride : 0;
+  p->max_position = r->max_position;
+  p->rot_begin = r->rot_begin;
+  p->rot_dim = r->rot_dim;
+  p->neighbours = r->neighbours;
+  p->n_axes = r->n_axes;
+  p->dealt = r->n_axes > 1 ? r->dealt : 0;
+  for (int a = 0; a < r->n_axes && r->n_axes > 1; ++a) p->sections[a] = r->sections[a];
+  return FLEX_OK;
+}
+
+// Queries of an append: read at q_stride, written contiguous. In place only
+// when the rows are the same; any other overlap would race.
+int check_queries(const flex_attn_shape& sh, const void* q, int64_t q_stride, const void* q_out, int64_t n_tokens) {
+  const int64_t row = int64_t(sh.num_q_heads) * sh.head_dim_qk;
+  if (!q || !q_out || !aligned16(q) || !aligned16(q_out))
+    return set_error(FLEX_ERR_INVALID_ARG, "q and q_out must be non-NULL and 16-byte aligned");
+  if (q_stride < row || q_stride % 8)
+    return set_error(FLEX_ERR_INVALID_ARG, "q_stride must cover Hq * d_qk and be a 16-byte multiple");
+  const uintptr_t a = reinterpret_cast<uintptr_t>(q), b = reinterpret_cast<uintptr_t>(q_out);
+  const uintptr_t a_end = a + 2 * uintptr_t((n_tokens - 1) * q_stride + row), b_end = b + 2 * uintptr_t(n_tokens * row);
+  if (a < b_end && b < a_end && !(a == b && (q_stride == row || n_tokens == 1)))
+    return set_error(FLEX_ERR_INVALID_ARG, "q_out overlaps q (in place needs q_out == q and q_stride == Hq * d_qk)");
+  return FLEX_OK;
+}
+
+}  // namespace
+
+extern "C" int flex_attn_kv_append(const flex_attn_shape* shape, const flex_attn_append_args* a, void* stream) {
+  clear_error();
+  if (!shape || !a) return set_error(FLEX_ERR_INVALID_ARG, "shape or args is NULL");
+  if (const int st = check_shape(*shape); st != FLEX_OK) return st;
+  if (a->n_tokens < 0) return set_error(FLEX_ERR_INVALID_ARG, "n_tokens < 0");
+  if (a->n_tokens == 0) return FLEX_OK;
+  AppendParams p;
+  if (const int st = prepare_append(shape, a, &p); st != FLEX_OK) return st;
   const hipError_t e = launch_kv_append(p, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? FLEX_OK : hip_fail(e, "kv append launch");
+}
+
+extern "C" int flex_attn_rope_append(const flex_attn_shape* shape, const flex_attn_rope* rope,
+                                     const flex_attn_rope_append_args* a, void* stream) {
+  clear_error();
+  if (!shape || !rope || !a) return set_error(FLEX_ERR_INVALID_ARG, "shape, rope or args is NULL");
+  if (const int st = check_shape(*shape); st != FLEX_OK) return st;
+  const int64_t n = a->kv.n_tokens;
+  if (n < 0) return set_error(FLEX_ERR_INVALID_ARG, "n_tokens < 0");
+  if (n == 0) return FLEX_OK;
+  RopeAppendParams p{};
+  if (const int st = prepare_append(shape, &a->kv, &p.kv); st != FLEX_OK) return st;
+  if (const int st = prepare_rope(*shape, rope, n, false, &p.rope); st != FLEX_OK) return st;
+  if (const int st = check_queries(*shape, a->q, a->q_stride, a->q_out, n); st != FLEX_OK) return st;
+  p.q = static_cast<const uint16_t*>(a->q);
+  p.q_stride = a->q_stride;
+  p.q_out = static_cast<uint16_t*>(a->q_out);
+  p.Hq = shape->num_q_heads;
+  p.Hkv = shape->num_kv_heads;
+  const hipError_t e = launch_rope_append(p, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? FLEX_OK : hip_fail(e, "rope append launch");
+}
+
+extern "C" int flex_attn_kv8_append(const flex_attn_shape* shape, const flex_attn_rope* rope,
+                                    const flex_attn_kv8_append_args* a, void* stream) {
+  clear_error();
+  if (!shape || !a) return set_error(FLEX_ERR_INVALID_ARG, "shape or args is NULL");
+  if (const int st = check_shape(*shape); st != FLEX_OK) return st;
+  const int64_t n = a->n_tokens, Hkv = shape->num_kv_heads, d = shape->head_dim_qk;
+  if (shape->v_aliases_k || d != shape->head_dim_v)
+    return set_error(FLEX_ERR_UNSUPPORTED, "8-bit caches hold grouped-query heads of 64 or 128 only");
+  if (n < 0 || a->num_seqs < 0) return set_error(FLEX_ERR_INVALID_ARG, "n_tokens or num_seqs < 0");
+  if (n == 0 || a->num_seqs == 0) return FLEX_OK;
+  if (n > INT32_MAX) return set_error(FLEX_ERR_UNSUPPORTED, "n_tokens beyond 2^31 - 1");
+  if (!a->k_new || !a->v_new || !a->k_cache || !a->v_cache || !a->block_table || !a->seq_lens || !a->query_start_loc)
+    return set_error(FLEX_ERR_INVALID_ARG, "a required pointer is NULL");
+  if (!aligned16(a->k_new) || !aligned16(a->v_new) || !aligned16(a->k_cache) || !aligned16(a->v_cache))
+    return set_error(FLEX_ERR_INVALID_ARG, "new rows and caches must be 16-byte aligned");
+  if (a->k_new_stride < Hkv * d || a->k_new_stride % 8 || a->v_new_stride < Hkv * d || a->v_new_stride % 8)
+    return set_error(FLEX_ERR_INVALID_ARG, "new-row strides must cover Hkv * d and be 16-byte multiples");
+  for (int i = 0; i < 3; ++i) {
+    if (a->k_stride[i] <= 0 || a->v_stride[i] <= 0 || a->k_stride[i] % 16 || a->v_stride[i] % 16)
+      return set_error(FLEX_ERR_INVALID_ARG, "cache strides must be positive multiples of 16 bytes");
+  }
+  if (a->k_stride[2] < d || a->v_stride[2] < d)
+    return set_error(FLEX_ERR_INVALID_ARG, "cache head stride smaller than the head dimension");
+  if (a->num_pages <= 0) return set_error(FLEX_ERR_INVALID_ARG, "num_pages must be positive");
+  if (a->block_table_stride < 1) return set_error(FLEX_ERR_INVALID_ARG, "block_table_stride must be positive");
+  if (const int st = check_scales(*shape, a->kv_scales, a->scale_page_stride); st != FLEX_OK) return st;
+  Kv8AppendParams p{};
+  if (rope) {
+    if (const int st = prepare_rope(*shape, rope, n, true, &p.rope); st != FLEX_OK) return st;
+    if (const int st = check_queries(*shape, a->q, a->q_stride, a->q_out, n); st != FLEX_OK) return st;
+    p.q = static_cast<const uint16_t*>(a->q);
+    p.q_stride = a->q_stride;
+    p.q_out = static_cast<uint16_t*>(a->q_out);
+  }
+  p.k_new = static_cast<const uint16_t*>(a->k_new);
+  p.v_new = static_cast<const uint16_t*>(a->v_new);
+  p.k_new_stride = a->k_new_stride;
+  p.v_new_stride = a->v_new_stride;
+  p.n_tokens = n;
+  p.bt = a->block_table;
+  p.seq_lens = a->seq_lens;
+  p.qsl = a->query_start_loc;
+  p.bt_stride = a->block_table_stride;
+  p.num_seqs = a->num_seqs;
+  p.Hq = shape->num_q_heads;
+  p.Hkv = shape->num_kv_heads;
+  p.P = shape->page_size;
+  p.k = static_cast<uint8_t*>(a->k_cache);
+  p.v = static_cast<uint8_t*>(a->v_cache);
+  p.k_sp = a->k_stride[0];
+  p.k_ss = a->k_stride[1];
+  p.k_sh = a->k_stride[2];
+  p.v_sp = a->v_stride[0];
+  p.v_ss = a->v_stride[1];
+  p.v_sh = a->v_stride[2];
+  p.scales = static_cast<uint8_t*>(a->kv_scales);
+  p.scale_sp = a->scale_page_stride;
+  p.num_pages = a->num_pages;
+  p.bad_count = a->bad_count;
+  const hipError_t e = launch_kv8_append(p, int(d), static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? FLEX_OK : hip_fail(e, "8-bit append launch");
 }

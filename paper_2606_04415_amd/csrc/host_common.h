@@ -91,6 +91,9 @@ constexpr double kPrefillLaunchSec = 10e-6;
 // tail only when its predicted prefill phase lasts at least this long.
 constexpr double kTailMinPrefillUs = 100.0;
 
+// Tokens that share one scale of an 8-bit cache (pages hold whole blocks).
+constexpr int kKv8Block = 16;
+
 // Rows (query heads) one decode work-group owns in the 576/512 layout.
 constexpr int kLatentRowsPerWG = 64;       // latent heads must be a multiple of this
 constexpr int kLatentRowsPerWGWide = 128;  // heads per latent decode work-group when they divide
@@ -108,6 +111,7 @@ struct flex_attn_plan {
   flex_attn_plan_info info;
   int32_t cus_total;        // the CU count the plan was partitioned against
   int32_t rows_per_wg;      // query rows of one decode work-group
+  int32_t kv_bits;          // 16: bf16 caches, 8: e4m3 caches with block scales
   int32_t max_pages_per_seq;  // block-table entries a row must hold
   std::vector<int32_t> words;
 };

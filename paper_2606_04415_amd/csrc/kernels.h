@@ -9,7 +9,7 @@ namespace flexattn {
 
 struct CacheRef {
   const uint16_t* base;
-  int64_t sp, ss, sh;  // element strides: page, slot, kv head
+  int64_t sp, ss, sh;  // element strides: page, slot, kv head (8-bit caches: bytes)
 };
 
 struct AttnParams {
@@ -37,6 +37,8 @@ struct AttnParams {
   int32_t grid_y;
   int32_t xcd_remap;      // prefill: 1-D grid mapped so each XCD serves one column
   float scale_log2;       // sm_scale * log2(e)
+  const uint8_t* kv_scales;   // 8-bit caches: scale bytes, [page][block of 16 slots][kv head][K, V]
+  int64_t scale_sp;           // bytes from page to page
 };
 
 // Allow a kernel the dynamic LDS it launches with. The attribute is set on
@@ -88,5 +90,50 @@ struct AppendParams {
 };
 
 hipError_t launch_kv_append(const AppendParams& a, hipStream_t stream);
+
+constexpr int kRopeMaxAxes = 4;
+struct RopeParams {
+  const float* cos_sin;                 // [max_position][rot_dim]; nullptr: no rotation
+  const int32_t* positions;             // [n_axes][n_tokens]; nullptr: the tokens' own
+  int64_t positions_stride;
+  int32_t max_position, rot_begin, rot_dim, neighbours, n_axes, dealt;
+  int32_t sections[kRopeMaxAxes];
+};
+
+struct RopeAppendParams {
+  AppendParams kv;
+  const uint16_t* q;
+  int64_t q_stride;                     // elements per token row
+  uint16_t* q_out;                      // contiguous
+  int32_t Hq, Hkv;
+  int32_t per_wg;                       // tokens of one work-group
+  RopeParams rope;
+};
+
+hipError_t launch_rope_append(const RopeAppendParams& p, hipStream_t stream);
+
+struct Kv8AppendParams {
+  const uint16_t* k_new;
+  const uint16_t* v_new;
+  const uint16_t* q;
+  int64_t k_new_stride, v_new_stride, q_stride;   // elements per token row
+  uint16_t* q_out;
+  int64_t n_tokens;
+  const int32_t* bt;
+  const int32_t* seq_lens;
+  const int32_t* qsl;
+  int32_t bt_stride, num_seqs;
+  int32_t Hq, Hkv, P;
+  uint8_t* k;                           // caches: byte strides of page, slot and head
+  uint8_t* v;
+  int64_t k_sp, k_ss, k_sh, v_sp, v_ss, v_sh;
+  uint8_t* scales;
+  int64_t scale_sp;
+  int64_t num_pages;
+  int32_t* bad_count;
+  RopeParams rope;
+};
+
+hipError_t launch_kv8_append(const Kv8AppendParams& p, int head_dim, hipStream_t stream);
 
 }  // namespace flexattn

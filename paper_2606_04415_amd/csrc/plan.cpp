@@ -146,6 +146,14 @@ extern "C" int flex_attn_plan(const flex_attn_shape* shape, const flex_attn_plan
   if (cus_total < 1 || wg_per_cu < 1 || min_tokens < 1 || granule < 1)
     return set_error(FLEX_ERR_INVALID_ARG, "plan options must be positive");
   if (o.decode_tail < -1 || o.decode_tail > 0) return set_error(FLEX_ERR_INVALID_ARG, "decode_tail must be 0 or -1");
+  if (o.kv_bits != 0 && o.kv_bits != 8 && o.kv_bits != 16)
+    return set_error(FLEX_ERR_INVALID_ARG, "kv_bits must be 0, 8 or 16");
+  const bool kv8 = o.kv_bits == 8;
+  if (kv8 && (latent || split))
+    return set_error(FLEX_ERR_UNSUPPORTED, "8-bit caches hold grouped-query heads of 64 or 128 only");
+  if (kv8 && bm != 0 && bm != 128)
+    return set_error(FLEX_ERR_UNSUPPORTED, "8-bit caches take prefill tiles of 128 flattened rows only");
+  if (kv8) bm = 128;
   if (o.cus_decode < -1 || o.cus_decode > cus_total)
     return set_error(FLEX_ERR_INVALID_ARG, "cus_decode must be -1, 0 or in [1, cus_total]");
   if (latent ? (bm != 64 && bm != 128) : split ? bm != 128 : (bm != 0 && bm != 16 && bm != 32 && bm != 128))
@@ -188,8 +196,13 @@ extern "C" int flex_attn_plan(const flex_attn_shape* shape, const flex_attn_plan
   // Algorithmic work of each phase (feeds the cost model and the plan info).
   const int64_t kv_row = int64_t(sh.num_kv_heads) * 2 *
                          (sh.v_aliases_k ? sh.head_dim_qk : sh.head_dim_qk + sh.head_dim_v);
+  // Cache bytes of the first `tokens` keys: rows of two bytes a value, or of
+  // one with two scale bytes for each 16 tokens and head.
+  auto kv_bytes = [&](int64_t tokens) -> int64_t {
+    return kv8 ? tokens * (kv_row / 2) + cdiv(tokens, kKv8Block) * sh.num_kv_heads * 2 : tokens * kv_row;
+  };
   int64_t dec_bytes = 0;
-  for (int32_t s : dec) dec_bytes += int64_t(seq_lens[s]) * kv_row;
+  for (int32_t s : dec) dec_bytes += kv_bytes(seq_lens[s]);
   int64_t pre_flops = 0;
   for (int32_t s : pre) {
     const int64_t n = qsl[s + 1] - qsl[s], L = seq_lens[s];
@@ -445,6 +458,7 @@ extern "C" int flex_attn_plan(const flex_attn_shape* shape, const flex_attn_plan
   if (!plan) return set_error(FLEX_ERR_INTERNAL, "out of host memory");
   plan->shape = sh;
   plan->rows_per_wg = rows_per_wg;
+  plan->kv_bits = kv8 ? 8 : 16;
   plan->cus_total = int32_t(cus_total);
   plan->max_pages_per_seq = max_pages_per_seq;
   const int32_t n_pre_items = int32_t(tiles.size());
@@ -532,7 +546,7 @@ extern "C" int flex_attn_plan(const flex_attn_shape* shape, const flex_attn_plan
   info.n_fused_wgs = int32_t(fused.size());
   info.n_decode_tail_ranges = int32_t(RB);
   for (size_t i = size_t(ranges[RA]); i < pieces.size(); ++i)
-    info.decode_tail_bytes += double(pieces[i].k1 - pieces[i].k0) * double(kv_row);
+    info.decode_tail_bytes += double(kv_bytes(pieces[i].k1 - pieces[i].k0));   // (pieces start on a page)
   if (log_level() > 0) log_plan(*plan);
   *out_plan = plan;
   return FLEX_OK;

@@ -33,6 +33,8 @@ EXPORTED = [
     "flex_attn_corun_streams", "flex_attn_corun_set_timing", "flex_attn_corun_timing_read",
     "flex_attn_debug_gather", "flex_attn_workspace_init", "flex_attn_kv_append",
     "flex_attn_mixed_static", "flex_attn_static_scratch_bytes", "flex_attn_validate_host", "flex_attn_set_debug",
+    "flex_attn_rope_append", "flex_attn_kv8_append", "flex_attn_decode_kv8", "flex_attn_prefill_kv8",
+    "flex_attn_mixed_kv8",
     "flex_ctl_create", "flex_ctl_destroy", "flex_ctl_set_profile", "flex_ctl_observe", "flex_ctl_decide",
     "flex_ctl_estimates", "flex_ts_create", "flex_ts_destroy", "flex_ts_next", "flex_ts_observe", "flex_ts_totals",
 ]
@@ -47,6 +49,7 @@ FLEX_CTL_FUSED_FASTER = 7
 FLEX_TS_DECODE = 0
 FLEX_TS_PREFILL = 1
 FLEX_TIMING_RING = 1024
+FLEX_ROPE_MAX_AXES = 4
 
 
 class Shape(ctypes.Structure):
@@ -61,7 +64,8 @@ class PlanOpts(ctypes.Structure):
                 ("min_split_tokens", ctypes.c_int32),
                 ("wg_per_cu", ctypes.c_int32), ("split_granule", ctypes.c_int32),
                 ("hbm_gbps", ctypes.c_double), ("decode_gbps_per_cu", ctypes.c_double),
-                ("prefill_tflops_per_cu", ctypes.c_double), ("decode_tail", ctypes.c_int32)]
+                ("prefill_tflops_per_cu", ctypes.c_double), ("decode_tail", ctypes.c_int32),
+                ("kv_bits", ctypes.c_int32)]
 
 
 class PlanInfo(ctypes.Structure):
@@ -95,6 +99,32 @@ class AppendArgs(ctypes.Structure):
                 ("v_new_stride", ctypes.c_int64), ("slot_mapping", ctypes.c_void_p), ("n_tokens", ctypes.c_int64),
                 ("k_cache", ctypes.c_void_p), ("k_stride", ctypes.c_int64 * 3), ("v_cache", ctypes.c_void_p),
                 ("v_stride", ctypes.c_int64 * 3), ("num_pages", ctypes.c_int64), ("bad_count", ctypes.c_void_p)]
+
+
+class Rope(ctypes.Structure):
+    _fields_ = [("cos_sin", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("positions_stride", ctypes.c_int64),
+                ("max_position", ctypes.c_int32), ("rot_begin", ctypes.c_int32), ("rot_dim", ctypes.c_int32),
+                ("neighbours", ctypes.c_int32), ("n_axes", ctypes.c_int32), ("dealt", ctypes.c_int32),
+                ("sections", ctypes.c_int32 * FLEX_ROPE_MAX_AXES)]
+
+
+class RopeAppendArgs(ctypes.Structure):
+    _fields_ = [("kv", AppendArgs), ("q", ctypes.c_void_p), ("q_stride", ctypes.c_int64), ("q_out", ctypes.c_void_p)]
+
+
+class Kv8AppendArgs(ctypes.Structure):
+    _fields_ = [("k_new", ctypes.c_void_p), ("v_new", ctypes.c_void_p), ("k_new_stride", ctypes.c_int64),
+                ("v_new_stride", ctypes.c_int64), ("q", ctypes.c_void_p), ("q_stride", ctypes.c_int64),
+                ("q_out", ctypes.c_void_p), ("n_tokens", ctypes.c_int64), ("num_seqs", ctypes.c_int32),
+                ("block_table", ctypes.c_void_p), ("block_table_stride", ctypes.c_int32),
+                ("seq_lens", ctypes.c_void_p), ("query_start_loc", ctypes.c_void_p), ("k_cache", ctypes.c_void_p),
+                ("k_stride", ctypes.c_int64 * 3), ("v_cache", ctypes.c_void_p), ("v_stride", ctypes.c_int64 * 3),
+                ("kv_scales", ctypes.c_void_p), ("scale_page_stride", ctypes.c_int64),
+                ("num_pages", ctypes.c_int64), ("bad_count", ctypes.c_void_p)]
+
+
+class Kv8Args(ctypes.Structure):
+    _fields_ = [("attn", Args), ("kv_scales", ctypes.c_void_p), ("scale_page_stride", ctypes.c_int64)]
 
 
 class CtlOpts(ctypes.Structure):
@@ -176,6 +206,11 @@ def lib():
     L.flex_attn_debug_gather.argtypes = [vp, ctypes.POINTER(Args), i32, i32, vp, vp, vp]
     L.flex_attn_workspace_init.argtypes = [vp, sz, vp]
     L.flex_attn_kv_append.argtypes = [ctypes.POINTER(Shape), ctypes.POINTER(AppendArgs), vp]
+    L.flex_attn_rope_append.argtypes = [ctypes.POINTER(Shape), ctypes.POINTER(Rope), ctypes.POINTER(RopeAppendArgs), vp]
+    L.flex_attn_kv8_append.argtypes = [ctypes.POINTER(Shape), ctypes.POINTER(Rope), ctypes.POINTER(Kv8AppendArgs), vp]
+    for f in ("flex_attn_decode_kv8", "flex_attn_prefill_kv8"):
+        getattr(L, f).argtypes = [vp, ctypes.POINTER(Kv8Args), vp]
+    L.flex_attn_mixed_kv8.argtypes = [vp, ctypes.POINTER(Kv8Args), ctypes.c_int, vp, vp]
     L.flex_ctl_create.argtypes = [ctypes.POINTER(CtlOpts), ctypes.POINTER(vp)]
     L.flex_ctl_destroy.argtypes = [vp]
     L.flex_ctl_destroy.restype = None
@@ -449,6 +484,235 @@ def flex_attn_kv_append(shape: Shape, args: AppendArgs, stream=None):
     check(lib().flex_attn_kv_append(ctypes.byref(shape), ctypes.byref(args), s), "flex_attn_kv_append")
 
 
+def _one_device(tensors):
+    """The device of the tensors given (None skipped); ValueError if there are several."""
+    devs = {t.device for t in tensors if t is not None}
+    _require(len(devs) == 1, f"tensors on several devices: {devs}")
+    return devs.pop()
+
+
+def _run(what, args, stream, *call):
+    """Calls lib().<what>(*call, stream) on the device of args' tensors, on its
+    current stream unless one is given. ValueError for tensors that are not on a GPU."""
+    import torch
+    _require(args.device.type == "cuda", f"{what} needs GPU tensors, not {args.device}")
+    with torch.cuda.device(args.device):
+        s = stream if stream is not None else current_stream()
+        check(getattr(lib(), what)(*call, s), what)
+
+
+def _rows(name, t, heads, dim, dtype=None):
+    """Checks a [tokens, heads, dim] tensor whose rows have no gaps; returns the token stride."""
+    import torch
+    _require(t.dtype == (dtype or torch.bfloat16), f"{name} must be {dtype or torch.bfloat16}, not {t.dtype}")
+    _require(t.dim() == 3 and tuple(t.shape[1:]) == (heads, dim), f"{name} must be [tokens, {heads}, {dim}]")
+    _require(t.shape[0] == 0 or ((dim == 1 or t.stride(2) == 1) and (heads == 1 or t.stride(1) == dim)),
+             f"{name} must have contiguous rows")
+    return t.stride(0) if t.shape[0] > 1 else heads * dim
+
+
+def _cache(name, t, heads, dtype):
+    _require(t.dtype == dtype, f"{name} must be {dtype}, not {t.dtype}")
+    _require(t.dim() == 4 and t.shape[2] == heads and t.stride(3) == 1,
+             f"{name} must be [pages, P, {heads}, d] with a unit innermost stride")
+    return (ctypes.c_int64 * 3)(*t.stride()[:3])
+
+
+def _index(name, t, shape=None):
+    import torch
+    _require(t.dtype == torch.int32, f"{name} must be int32, not {t.dtype}")
+    _require(t.is_contiguous(), f"{name} must be contiguous")
+    _require(shape is None or tuple(t.shape) == tuple(shape), f"{name} must be {list(shape or ())}")
+    return t.data_ptr()
+
+
+def rope_table(max_position: int, rot_dim: int, base: float = 10000.0, device="cuda"):
+    """fp32 [max_position, rot_dim] for make_rope: cosines, then sines, of the
+    angles p * base^(-2 i / rot_dim), worked out in 64 bits (in 32, the angles
+    of far positions are off by more than the table's rounding)."""
+    import torch
+    i = torch.arange(rot_dim // 2, dtype=torch.float64, device=device)
+    angle = torch.arange(max_position, dtype=torch.float64, device=device)[:, None] * float(base) ** (-2.0 * i / rot_dim)
+    return torch.cat([torch.cos(angle), torch.sin(angle)], 1).float()
+
+
+def make_rope(cos_sin, positions=None, rot_begin: int = 0, neighbours: bool = False, sections=None,
+              dealt: bool = False) -> Rope:
+    """Rope from device tensors: cos_sin fp32 [max_position, rot_dim] (rope_table),
+    positions int32 [tokens] or [axes, tokens] (rows may be apart), or None for
+    flex_attn_kv8_append with one axis. sections: pairs of each axis, given
+    when there is more than one."""
+    import torch
+    _require(cos_sin.dtype == torch.float32, f"cos_sin must be float32, not {cos_sin.dtype}")
+    _require(cos_sin.dim() == 2 and cos_sin.is_contiguous(), "cos_sin must be [max_position, rot_dim], contiguous")
+    r = Rope()
+    r.cos_sin = cos_sin.data_ptr()
+    r.max_position, r.rot_dim = cos_sin.shape
+    r.rot_begin, r.neighbours, r.dealt, r.n_axes = rot_begin, int(bool(neighbours)), int(bool(dealt)), 1
+    r.n_positions = None
+    if positions is not None:
+        _require(positions.dtype == torch.int32, f"positions must be int32, not {positions.dtype}")
+        p = positions[None] if positions.dim() == 1 else positions
+        _require(p.dim() == 2 and (p.shape[1] <= 1 or p.stride(1) == 1), "positions must be [axes, tokens] with unit column stride")
+        r.positions, r.n_axes, r.n_positions = p.data_ptr(), p.shape[0], p.shape[1]
+        r.positions_stride = p.stride(0) if p.shape[0] > 1 else p.shape[1]
+    axes = list(sections) if sections is not None else []
+    _require(len(axes) == (r.n_axes if r.n_axes > 1 else len(axes)) and len(axes) <= FLEX_ROPE_MAX_AXES,
+             f"sections must name the pairs of {r.n_axes} axes")
+    for a, n in enumerate(axes):
+        r.sections[a] = n
+    r.device = _one_device([cos_sin, positions])
+    return r
+
+
+def _check_rope(rope, args, n_tokens):
+    _require(rope.device == args.device, f"rope on {rope.device}, tensors on {args.device}")
+    _require(rope.n_positions is None or rope.n_positions >= n_tokens,
+             f"{rope.n_positions} positions for {n_tokens} tokens")
+
+
+def make_rope_append_args(q, q_out, k_new, v_new, slot_mapping, k_cache, v_cache, bad_count=None) -> RopeAppendArgs:
+    """RopeAppendArgs from device tensors: q [n, Hq, d_qk] with contiguous rows,
+    q_out [n, Hq, d_qk] contiguous (q itself to turn it in place), the rest as
+    for make_append_args (v_new and v_cache None when values alias keys)."""
+    import torch
+    n, (Hq, dk), Hkv = q.shape[0], q.shape[1:], k_cache.shape[2]
+    a = RopeAppendArgs()
+    a.q, a.q_stride, a.q_out = q.data_ptr(), _rows("q", q, Hq, dk), q_out.data_ptr()
+    _require(q_out.shape == q.shape and q_out.dtype == torch.bfloat16 and q_out.is_contiguous(),
+             "q_out must be like q, contiguous")
+    _require((v_new is None) == (v_cache is None), "v_new and v_cache are given together")
+    a.kv.k_new, a.kv.k_new_stride = k_new.data_ptr(), _rows("k_new", k_new, Hkv, dk)
+    a.kv.k_stride, a.kv.k_cache = _cache("k_cache", k_cache, Hkv, torch.bfloat16), k_cache.data_ptr()
+    a.kv.v_stride, a.kv.num_pages, a.kv.n_tokens = a.kv.k_stride, k_cache.shape[0], n
+    if v_new is not None:
+        a.kv.v_new, a.kv.v_new_stride = v_new.data_ptr(), _rows("v_new", v_new, Hkv, v_cache.shape[3])
+        a.kv.v_stride, a.kv.v_cache = _cache("v_cache", v_cache, Hkv, torch.bfloat16), v_cache.data_ptr()
+        _require(v_cache.shape[:2] == k_cache.shape[:2], "k_cache and v_cache must have the same pages")
+    a.kv.slot_mapping = _index("slot_mapping", slot_mapping, (n,))
+    _require(k_new.shape[0] == n and (v_new is None or v_new.shape[0] == n), "q, k_new and v_new must have the same tokens")
+    if bad_count is not None:
+        a.kv.bad_count = _index("bad_count", bad_count)
+    a.device = _one_device([q, q_out, k_new, v_new, slot_mapping, k_cache, v_cache, bad_count])
+    a.sizes = (Hq, Hkv, dk, None if v_new is None else v_cache.shape[3], k_cache.shape[1])
+    return a
+
+
+def _check_sizes(shape, args):
+    want = (shape.num_q_heads, shape.num_kv_heads, shape.head_dim_qk, None if shape.v_aliases_k else shape.head_dim_v,
+            shape.page_size)
+    _require(all(b is _ANY or a == b for a, b in zip(want, args.sizes)), f"tensors for {args.sizes}, shape {want}")
+
+
+_ANY = object()
+
+
+def flex_attn_rope_append(shape: Shape, rope: Rope, args: RopeAppendArgs, stream=None):
+    _check_sizes(shape, args)
+    _check_rope(rope, args, args.kv.n_tokens)
+    _run("flex_attn_rope_append", args, stream, ctypes.byref(shape), ctypes.byref(rope), ctypes.byref(args))
+
+
+def make_kv8_cache(num_pages: int, page_size: int, num_kv_heads: int, head_dim: int, device="cuda"):
+    """(k_cache, v_cache, kv_scales) of an empty 8-bit cache: e4m3 codes
+    [pages, P, Hkv, d] and e8m0 scales [pages, P / 16, Hkv, 2], all zero bytes."""
+    import torch
+    k, v = (torch.zeros((num_pages, page_size, num_kv_heads, head_dim), dtype=torch.uint8, device=device) for _ in "kv")
+    s = torch.zeros((num_pages, page_size // 16, num_kv_heads, 2), dtype=torch.uint8, device=device)
+    return k.view(torch.float8_e4m3fn), v.view(torch.float8_e4m3fn), s.view(torch.float8_e8m0fnu)
+
+
+def _check_kv8(k_cache, v_cache, kv_scales):
+    """Checks an 8-bit cache; returns (k strides, v strides, scale page stride)."""
+    import torch
+    pages, P, heads = k_cache.shape[:3]
+    ks = _cache("k_cache", k_cache, heads, torch.float8_e4m3fn)
+    vs = _cache("v_cache", v_cache, heads, torch.float8_e4m3fn)
+    _require(v_cache.shape == k_cache.shape, "k_cache and v_cache must have the same shape")
+    _require(kv_scales.dtype == torch.float8_e8m0fnu, f"kv_scales must be float8_e8m0fnu, not {kv_scales.dtype}")
+    _require(P % 16 == 0 and tuple(kv_scales.shape) == (pages, P // 16, heads, 2),
+             f"kv_scales must be [{pages}, {P} / 16, {heads}, 2]")
+    _require(kv_scales[0].is_contiguous(), "kv_scales must be contiguous within a page")
+    return ks, vs, kv_scales.stride(0) if pages > 1 else P // 16 * heads * 2
+
+
+def make_kv8_append_args(k_new, v_new, block_table, seq_lens, query_start_loc, k_cache, v_cache, kv_scales, q=None,
+                         q_out=None, bad_count=None) -> Kv8AppendArgs:
+    """Kv8AppendArgs from device tensors: k_new / v_new [n, Hkv, d] with
+    contiguous rows, the batch's block_table, seq_lens and query_start_loc as
+    the attention takes them, an 8-bit cache (make_kv8_cache), and q
+    [n, Hq, d] with q_out (contiguous, may be q) when a rotation is applied."""
+    import torch
+    n, B = k_new.shape[0], seq_lens.numel()
+    heads, d = k_cache.shape[2:]
+    a = Kv8AppendArgs()
+    a.k_stride, a.v_stride, a.scale_page_stride = _check_kv8(k_cache, v_cache, kv_scales)
+    a.k_new, a.k_new_stride = k_new.data_ptr(), _rows("k_new", k_new, heads, d)
+    a.v_new, a.v_new_stride = v_new.data_ptr(), _rows("v_new", v_new, heads, d)
+    _require(v_new.shape[0] == n, "k_new and v_new must have the same tokens")
+    _require((q is None) == (q_out is None), "q and q_out are given together")
+    Hq = _ANY
+    if q is not None:
+        Hq = q.shape[1]
+        a.q, a.q_stride, a.q_out = q.data_ptr(), _rows("q", q, Hq, d), q_out.data_ptr()
+        _require(q_out.shape == q.shape and q_out.dtype == torch.bfloat16 and q_out.is_contiguous(),
+                 "q_out must be like q, contiguous")
+        _require(q.shape[0] == n, "q and k_new must have the same tokens")
+    a.n_tokens, a.num_seqs, a.num_pages = n, B, k_cache.shape[0]
+    _require(block_table.dtype == torch.int32 and block_table.dim() == 2 and block_table.stride(1) == 1 and
+             block_table.shape[0] == B, "block_table must be int32 [sequences, pages] with unit column stride")
+    a.block_table = block_table.data_ptr()
+    a.block_table_stride = block_table.stride(0) if B > 1 else block_table.shape[1]
+    a.seq_lens, a.query_start_loc = _index("seq_lens", seq_lens, (B,)), _index("query_start_loc", query_start_loc, (B + 1,))
+    a.k_cache, a.v_cache, a.kv_scales = k_cache.data_ptr(), v_cache.data_ptr(), kv_scales.data_ptr()
+    if bad_count is not None:
+        a.bad_count = _index("bad_count", bad_count)
+    a.device = _one_device([k_new, v_new, block_table, seq_lens, query_start_loc, k_cache, v_cache, kv_scales, q, q_out,
+                            bad_count])
+    a.sizes = (Hq, heads, d, d, k_cache.shape[1])
+    return a
+
+
+def flex_attn_kv8_append(shape: Shape, rope: Optional[Rope], args: Kv8AppendArgs, stream=None):
+    _check_sizes(shape, args)
+    if rope is not None:
+        _check_rope(rope, args, args.n_tokens)
+    _run("flex_attn_kv8_append", args, stream, ctypes.byref(shape), ctypes.byref(rope) if rope is not None else None,
+         ctypes.byref(args))
+
+
+def make_kv8_args(q, k_cache, v_cache, kv_scales, block_table, seq_lens, query_start_loc, out, lse=None, d_plan=None,
+                  workspace=None) -> Kv8Args:
+    """Kv8Args from device tensors: as make_args, over an 8-bit cache (make_kv8_cache)."""
+    import torch
+    a = Kv8Args()
+    ks, vs, a.scale_page_stride = _check_kv8(k_cache, v_cache, kv_scales)
+    # the rest is checked as for a bf16 cache, with q standing in for it
+    a.attn = make_args(q, q[:0, None], q[:0, None], block_table, seq_lens, query_start_loc, out, lse, d_plan, workspace)
+    a.attn.k_cache, a.attn.v_cache, a.attn.k_stride, a.attn.v_stride = k_cache.data_ptr(), v_cache.data_ptr(), ks, vs
+    a.attn.num_pages = k_cache.shape[0]
+    a.kv_scales = kv_scales.data_ptr()
+    a.device = _one_device([q, k_cache, v_cache, kv_scales, lse, d_plan, workspace])
+    return a
+
+
+def flex_attn_decode_kv8(plan: Plan, args: Kv8Args, stream=None):
+    _run("flex_attn_decode_kv8", args, stream, plan.handle, ctypes.byref(args))
+
+
+def flex_attn_prefill_kv8(plan: Plan, args: Kv8Args, stream=None):
+    _run("flex_attn_prefill_kv8", args, stream, plan.handle, ctypes.byref(args))
+
+
+def flex_attn_mixed_kv8(plan: Plan, args: Kv8Args, mode: int, stream=None, corun: "Corun" = None):
+    import torch
+    _require(args.device.type == "cuda", f"flex_attn_mixed_kv8 needs GPU tensors, not {args.device}")
+    with torch.cuda.device(args.device):
+        s = stream if stream is not None else current_stream()
+        check(lib().flex_attn_mixed_kv8(plan.handle, ctypes.byref(args), mode, s,
+                                        corun.handle if corun is not None else None), "flex_attn_mixed_kv8")
+
+
 class Controller:
     """The online co-location controller (flex_ctl_*): observe steps, decide splits."""
 
@@ -594,6 +858,11 @@ class PagedAttention:
     def args(self, q, k_cache, v_cache, block_table, seq_lens, query_start_loc, out, lse=None) -> Args:
         return make_args(q, k_cache, v_cache, block_table, seq_lens, query_start_loc, out, lse,
                          self.d_plan, self.workspace)
+
+    def kv8_args(self, q, k_cache, v_cache, kv_scales, block_table, seq_lens, query_start_loc, out, lse=None) -> Kv8Args:
+        """Arguments of the calls over an 8-bit cache (a plan made with kv_bits=8)."""
+        return make_kv8_args(q, k_cache, v_cache, kv_scales, block_table, seq_lens, query_start_loc, out, lse,
+                             self.d_plan, self.workspace)
 
     def alloc_out(self, q, with_lse=False):
         import torch
