@@ -542,8 +542,8 @@ int flex_attn_kv8_append(const flex_attn_shape* shape, const flex_attn_rope* rop
 
 /* Attention over an 8-bit cache: flex_attn_decode, _prefill and _mixed with
  * cached values code * scale, on a plan made with kv_bits = 8. attn's caches
- * and strides are those of the 8-bit cache (strides in bytes); everything else
- * in it, outputs, workspace and debug mode included, is as for those calls.
+ * and strides are those of the 8-bit cache (strides in bytes, head strides
+ * below 2^31 as well); everything else in it, outputs, workspace and debug mode included, is as for those calls.
  * FLEX_MODE_FUSED is FLEX_ERR_UNSUPPORTED. A NaN in a value row reaches the
  * queries that attend it and may reach others of the same tile of 32 keys of
  * that sequence; slots past a sequence's end never count. */

@@ -98,6 +98,8 @@ int prepare(const flex_attn_plan_t* plan, const flex_attn_args* a, AttnParams* p
   if (a->k_stride[0] * esz >= lim || vs[0] * esz >= lim || a->k_stride[1] * esz * sh.page_size >= lim ||
       vs[1] * esz * sh.page_size >= lim)
     return set_error(FLEX_ERR_INVALID_ARG, "cache page stride or page_size * slot stride reaches 2^31 bytes");
+  if (kv8 && (a->k_stride[2] >= lim || vs[2] >= lim))
+    return set_error(FLEX_ERR_INVALID_ARG, "cache head stride reaches 2^31 bytes");
   if (kv8)
     if (const int st = check_scales(sh, kv8->kv_scales, kv8->scale_page_stride); st != FLEX_OK) return st;
   if (a->k_stride[2] < sh.head_dim_qk || vs[2] < (sh.v_aliases_k ? sh.head_dim_qk : sh.head_dim_v))

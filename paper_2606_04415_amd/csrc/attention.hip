@@ -25,6 +25,7 @@
 #include <mutex>
 #include <type_traits>
 
+#include "decode_walk.h"
 #include "device_common.h"
 #include "kernels.h"
 #include "latent_tile.h"
@@ -109,84 +110,6 @@ __global__ __launch_bounds__(256) void merge_kernel(AttnParams p) {
 // every gather into two serial memory round trips).
 constexpr int kPageWin = 512;
 
-// The running max of a row moves only when a chunk raises it by more than
-// this many log2 units; in between, probabilities are taken against the
-// stale max (so they stay below 2^8) and the accumulators are left alone.
-constexpr float kRescaleThreshold = 8.0f;
-
-__device__ __forceinline__ bool wave_any(bool pred) { return __builtin_amdgcn_ballot_w64(pred) != 0; }
-
-// Online-softmax step of one 16-row block over one chunk of NB 16-key blocks.
-// s[b][r]: raw score q.k of key kc0 + 16b + 4gq + r for this lane's row; with
-// `masked`, keys at or past `limit` are excluded (one code path: a second
-// inlined copy for the unmasked case costs registers). The scale is folded
-// into the exponent: p = 2^(s * scale_log2 - m). Updates the row's max m
-// (log2 units, lazily), the lane's partial sum l and the accumulators o
-// (rows 4gq + r), and gives the probabilities as bf16 A operands of P V, one
-// per 32 keys.
-template <int NB, int NACC>
-__device__ __forceinline__ void softmax_chunk(const f32x4 (&s)[NB], bool masked, int kc0, int limit, int gq,
-                                              float scale_log2, float& m, float& l, f32x4 (&o)[NACC],
-                                              u32x4 (&pop)[NB / 2]) {
-  float x[4 * NB];
-#pragma unroll
-  for (int e = 0; e < 4 * NB; ++e) x[e] = s[e >> 2][e & 3];
-  if (masked) {
-#pragma unroll
-    for (int e = 0; e < 4 * NB; ++e) x[e] = kc0 + chunk_key(e, gq) < limit ? x[e] : -INFINITY;
-  }
-  float bmax[NB / 2];
-#pragma unroll
-  for (int h = 0; h < NB / 2; ++h)
-    bmax[h] = fmaxf(fmaxf(fmaxf(x[8 * h], x[8 * h + 1]), fmaxf(x[8 * h + 2], x[8 * h + 3])),
-                    fmaxf(fmaxf(x[8 * h + 4], x[8 * h + 5]), fmaxf(x[8 * h + 6], x[8 * h + 7])));
-  float cmax = bmax[0];
-#pragma unroll
-  for (int h = 1; h < NB / 2; ++h) cmax = fmaxf(cmax, bmax[h]);
-  cmax = group_max(cmax) * scale_log2;
-  const bool need = cmax > m + kRescaleThreshold;
-  if (wave_any(need)) {
-    const float m_new = need ? cmax : m;
-    const float alpha = fast_exp2(m - m_new);   // 1 if unchanged, 0 from -inf
-    l *= alpha;
-    m = m_new;
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const float ar = shfl_f(alpha, 4 * gq + r);
-#pragma unroll
-      for (int a = 0; a < NACC; ++a) o[a][r] *= ar;
-    }
-  }
-  const float neg_m = m == -INFINITY ? 0.f : -m;
-  float psum = 0.f;
-#pragma unroll
-  for (int e2 = 0; e2 < 2 * NB; ++e2) {
-    const float p0 = fast_exp2(fmaf(x[2 * e2], scale_log2, neg_m));
-    const float p1 = fast_exp2(fmaf(x[2 * e2 + 1], scale_log2, neg_m));
-    psum += p0 + p1;
-    pop[e2 >> 2][e2 & 3] = pack_bf16x2(p0, p1);
-  }
-  l += psum;
-}
-
-// A block scale byte (e8m0) as the float whose exponent it is.
-__device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float((byte & 0xFFu) << 23); }
-
-// Two e4m3 codes (the low or high half of w) times a power of two, as two bf16
-// in one dword: exact, a code has 4 significant bits.
-template <bool HI>
-__device__ __forceinline__ uint32_t codes_bf16x2(uint32_t w, float scale) {
-  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, HI));
-}
-// Eight codes as eight bf16.
-__device__ __forceinline__ u32x4 codes_bf16x8(uint32_t w0, uint32_t w1, float scale) {
-  return u32x4{codes_bf16x2<false>(w0, scale), codes_bf16x2<true>(w0, scale), codes_bf16x2<false>(w1, scale),
-               codes_bf16x2<true>(w1, scale)};
-}
-// Bytes of two dwords paired up: (x0, y0, x1, y1) and (x2, y2, x3, y3).
-__device__ __forceinline__ uint32_t bytes_lo(uint32_t x, uint32_t y) { return __builtin_amdgcn_perm(y, x, 0x05010400u); }
-__device__ __forceinline__ uint32_t bytes_hi(uint32_t x, uint32_t y) { return __builtin_amdgcn_perm(y, x, 0x07030602u); }
-
 // ---------------------------------------------------------------------------
 // Decode, grouped-query heads.
 //
@@ -222,47 +145,25 @@ struct DecodeChunk {
   VRow v[8];        // value dims DPL*n .. of the lane's 8 keys
 };
 
-// The same chunk of an 8-bit cache: twice the keys in the same bytes. K loads
-// cover 8 keys x 128 bytes (head dim 128) or 16 keys x 64, V loads 4 keys; the
-// keys' operands are converted after the LDS, the values' after their bytes are
-// paired up by key.
-template <int D>
-struct DecodeChunk8 {
-  static constexpr int KL = D / 64;   // K loads of a 16-key block
-  using VRow = typename std::conditional<D == 128, u32x2, uint32_t>::type;
-  u32x4 k[4][KL];
-  VRow v[4][4];       // value dims DPL*n .. of keys 16b + 4gq + e
-  uint32_t scales;    // lane l: key and value scale byte of block l & 3
-};
-
-// Bytes of one wave's K staging buffer (32 keys, or 64 of an 8-bit cache).
+// Bytes of one wave's K staging buffer (32 keys).
 template <int D>
 constexpr int decode_kstage_bytes() { return 32 * D * 2; }
 
 // Physical 16-byte chunk of logical chunk x in key row r of a K staging
 // buffer: reads of one chunk by the 16 lanes of a lane group, and the
 // whole-line writes, hit 16 distinct 16-byte bank groups.
-template <int D>   // half the bytes of a row
+template <int D>
 __device__ __forceinline__ int decode_kswz(int x, int r) {
   if constexpr (D == 128) return x ^ (r & 15);
-  else if constexpr (D == 64) return x ^ ((r >> 1) & 7);
-  else return x ^ ((r >> 2) & 3);
+  else return x ^ ((r >> 1) & 7);
 }
-
-// Position in a wave's chunk stream: piece i (plan item), chunk ci of it, and
-// the piece's first entry in the LDS page window. Wave-uniform.
-struct DecodeCursor {
-  int i, ci, seq, k0, k1, poff;
-};
-
-__device__ __forceinline__ int pages_in(int k0, int k1, int P) { return (k1 - 1) / P - k0 / P + 1; }
 
 // One decode work-group's work: balanced range `range` (-1: none) of the
 // plan, column `col` of W, with threads tid = 0 .. NW*64-1, the range's
 // block-table window at s_pt and NW K staging buffers at s_kst (16-byte
 // aligned). Every call passes exactly one work-group barrier (two or more
 // per piece with COMBINE).
-template <int D, int NW, int P, bool COMBINE, bool NT, bool KV8 = false>
+template <int D, int NW, int P, bool COMBINE, bool NT>
 __device__ __forceinline__ void decode_gqa_body(const AttnParams& p, int range, int col, int W, int tid,
                                                 int* s_pt, uint8_t* s_kst) {
   // K/V loads marked non-temporal (read once, never reused): 7% faster on a
@@ -271,9 +172,7 @@ __device__ __forceinline__ void decode_gqa_body(const AttnParams& p, int range, 
   static_assert(D == 64 || D == 128, "head dim");
   constexpr int DC = D / 32;   // 32-dim chunks of the QK^T contraction
   constexpr int DPL = D / 16;  // value dims each lane owns in PV
-  constexpr int CK = KV8 ? 64 : 32;       // keys of a chunk
-  constexpr uint32_t ESZ = KV8 ? 1 : 2;   // bytes of a cached value
-  using Chunk = typename std::conditional<KV8, DecodeChunk8<D>, DecodeChunk<D>>::type;
+  using Chunk = DecodeChunk<D>;
   const int lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 15, gq = lane >> 4;
@@ -286,28 +185,25 @@ __device__ __forceinline__ void decode_gqa_body(const AttnParams& p, int range, 
   const int i_begin = range >= 0 ? p.ranges[range] : 0, i_end = range >= 0 ? p.ranges[range + 1] : 0;
   // Byte strides (the host checks that a page's slots span less than 2^31
   // bytes) and per-lane byte offsets of a chunk's loads from the page bases.
-  const uint8_t* kbase_b = reinterpret_cast<const uint8_t*>(p.kc.base) + int64_t(active ? g : 0) * p.kc.sh * ESZ;
-  const uint8_t* vbase_b = reinterpret_cast<const uint8_t*>(p.vc.base) + int64_t(active ? g : 0) * p.vc.sh * ESZ;
-  const uint32_t ksp_b = uint32_t(p.kc.sp) * ESZ, kss_b = uint32_t(p.kc.ss) * ESZ;
-  const uint32_t vsp_b = uint32_t(p.vc.sp) * ESZ, vss_b = uint32_t(p.vc.ss) * ESZ;
-  const uint32_t v_lane = uint32_t(4 * gq) * vss_b + ESZ * DPL * n;
+  const uint8_t* kbase_b = reinterpret_cast<const uint8_t*>(p.kc.base + int64_t(active ? g : 0) * p.kc.sh);
+  const uint8_t* vbase_b = reinterpret_cast<const uint8_t*>(p.vc.base + int64_t(active ? g : 0) * p.vc.sh);
+  const uint32_t ksp_b = uint32_t(p.kc.sp) * 2u, kss_b = uint32_t(p.kc.ss) * 2u;
+  const uint32_t vsp_b = uint32_t(p.vc.sp) * 2u, vss_b = uint32_t(p.vc.ss) * 2u;
+  const uint32_t v_lane = uint32_t(4 * gq) * vss_b + 2u * DPL * n;
   // K load t of a 16-key block: key kkey, 16-byte chunk kchunk of that key's
   // row (global byte offset k_lane[t], staging offset k_wr[t]); operand read
   // cc: key n, chunk 4cc + gq (staging offset k_rd[cc]).
-  // (8-bit: a row has D / 16 chunks of 16 codes; chunk 4t + gq of key n feeds
-  // two products, codes 0 .. 7 and 8 .. 15.)
-  constexpr int KROW = int(ESZ) * D;
-  constexpr int KT = KV8 ? D / 64 : DC;   // K loads of a 16-key block, and operand reads of a key
+  constexpr int KROW = 2 * D;
   uint8_t* const kst = s_kst + w * decode_kstage_bytes<D>();
-  uint32_t k_lane[KT], k_wr[KT], k_rd[KT];
+  uint32_t k_lane[DC], k_wr[DC], k_rd[DC];
 #pragma unroll
-  for (int t = 0; t < KT; ++t) {
+  for (int t = 0; t < DC; ++t) {
     const int q8 = lane >> 3, x8 = lane & 7;
-    const int kkey = KV8 ? (D == 128 ? 8 * t + q8 : lane >> 2) : D == 128 ? 8 * (t & 1) + q8 : 8 * t + q8;
-    const int kchunk = KV8 ? (D == 128 ? x8 : lane & 3) : D == 128 ? 8 * ((t >> 1) ^ (q8 & 1)) + x8 : x8;
+    const int kkey = D == 128 ? 8 * (t & 1) + q8 : 8 * t + q8;
+    const int kchunk = D == 128 ? 8 * ((t >> 1) ^ (q8 & 1)) + x8 : x8;
     k_lane[t] = uint32_t(kkey) * kss_b + 16u * uint32_t(kchunk);
-    k_wr[t] = uint32_t(kkey * KROW + 16 * decode_kswz<KROW / 2>(kchunk, kkey));
-    k_rd[t] = uint32_t(n * KROW + 16 * decode_kswz<KROW / 2>(4 * t + gq, n));
+    k_wr[t] = uint32_t(kkey * KROW + 16 * decode_kswz<D>(kchunk, kkey));
+    k_rd[t] = uint32_t(n * KROW + 16 * decode_kswz<D>(4 * t + gq, n));
   }
   __shared__ float s_m[NW][16];
   __shared__ float s_l[NW][16];
@@ -329,7 +225,7 @@ __device__ __forceinline__ void decode_gqa_body(const AttnParams& p, int range, 
   auto open = [&](DecodeCursor& c, int i, int poff) {
     for (; active && i < i_end; ++i) {
       const int k0 = scalar_word(p.items, 8 * i + 3), k1 = scalar_word(p.items, 8 * i + 4);
-      if (u * CK < k1 - k0) {
+      if (u * 32 < k1 - k0) {
         c = DecodeCursor{i, u, scalar_word(p.items, 8 * i), k0, k1, poff};
         return;
       }
@@ -339,7 +235,7 @@ __device__ __forceinline__ void decode_gqa_body(const AttnParams& p, int range, 
   };
   auto advance = [&](DecodeCursor& c) {
     c.ci += WPH;
-    if (c.k0 + CK * c.ci >= c.k1) open(c, c.i + 1, c.poff + pages_in(c.k0, c.k1, P));
+    if (c.k0 + 32 * c.ci >= c.k1) open(c, c.i + 1, c.poff + pages_in(c.k0, c.k1, P));
   };
 
   // K/V loads of one chunk through buffer resources built per 16-key half
@@ -351,20 +247,10 @@ __device__ __forceinline__ void decode_gqa_body(const AttnParams& p, int range, 
   // wait as if none had been issued).
   auto load = [&](Chunk& c, const DecodeCursor& cur) {
     const bool live = cur.i < i_end;
-    const int kc0 = cur.k0 + CK * cur.ci;
-    constexpr int NBLK = CK / 16;
-    __amdgpu_buffer_rsrc_t kr[NBLK], vr[NBLK];
-    if constexpr (KV8) {
-      // Lane l reads the scale pair of block l & 3: the block of the cursor's
-      // last key for those past it, the first pair of all past the range.
-      const int key = min(kc0 + 16 * (lane & 3), cur.k1 - 1);
-      const int64_t at = live ? int64_t(s_pt[cur.poff + key / P - cur.k0 / P]) * p.scale_sp +
-                                    (key % P / 16 * p.Hkv + (active ? g : 0)) * 2
-                              : 0;
-      c.scales = *reinterpret_cast<const uint16_t*>(p.kv_scales + at);
-    }
+    const int kc0 = cur.k0 + 32 * cur.ci;
+    __amdgpu_buffer_rsrc_t kr[2], vr[2];
 #pragma unroll
-    for (int b = 0; b < NBLK; ++b) {
+    for (int b = 0; b < 2; ++b) {
       const int key = kc0 + 16 * b;
       // (readfirstlane keeps resources in scalar registers: one the compiler
       // sees in vector registers becomes a loop.)
@@ -378,22 +264,10 @@ __device__ __forceinline__ void decode_gqa_body(const AttnParams& p, int range, 
                                                 0, __builtin_amdgcn_readfirstlane(int(nvalid * vss_b)), kBufferFlags);
     }
 #pragma unroll
-    for (int b = 0; b < NBLK; ++b)
+    for (int b = 0; b < 2; ++b)
 #pragma unroll
-      for (int cc = 0; cc < KT; ++cc)
+      for (int cc = 0; cc < DC; ++cc)
         c.k[b][cc] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(kr[b], int(k_lane[cc]), 0, kLoadAux));
-    if constexpr (KV8) {
-#pragma unroll
-      for (int b = 0; b < NBLK; ++b)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int off = int(v_lane + uint32_t(e) * vss_b);
-          if constexpr (D == 128)
-            c.v[b][e] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(vr[b], off, 0, kLoadAux));
-          else
-            c.v[b][e] = __builtin_amdgcn_raw_buffer_load_b32(vr[b], off, 0, kLoadAux);
-        }
-    } else
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const int off = int(v_lane + uint32_t(e & 3) * vss_b);
@@ -411,15 +285,9 @@ __device__ __forceinline__ void decode_gqa_body(const AttnParams& p, int range, 
   auto load_q = [&](int i) {
     const int tok = scalar_word(p.items, 8 * i + 6);
     const bool ok = n < G;
-    if constexpr (KV8) {   // operand 2t + h: dims 16 (4t + gq) + 8h .., as the codes of chunk 4t + gq
-      const uint16_t* qr = p.q + (int64_t(tok) * p.Hq + g * G + (ok ? n : 0)) * D + 16 * gq;
+    const uint16_t* qr = p.q + (int64_t(tok) * p.Hq + g * G + (ok ? n : 0)) * D + 8 * gq;
 #pragma unroll
-      for (int c = 0; c < DC; ++c) qop[c] = ok ? load16(qr + 64 * (c >> 1) + 8 * (c & 1)) : zero4();
-    } else {
-      const uint16_t* qr = p.q + (int64_t(tok) * p.Hq + g * G + (ok ? n : 0)) * D + 8 * gq;
-#pragma unroll
-      for (int c = 0; c < DC; ++c) qop[c] = ok ? load16(qr + 32 * c) : zero4();
-    }
+    for (int c = 0; c < DC; ++c) qop[c] = ok ? load16(qr + 32 * c) : zero4();
     q_piece = i;
   };
 
@@ -429,74 +297,32 @@ __device__ __forceinline__ void decode_gqa_body(const AttnParams& p, int range, 
   for (int a = 0; a < DPL; ++a) o[a] = f32x4{0.f, 0.f, 0.f, 0.f};
 
   auto compute = [&](const Chunk& c, const DecodeCursor& cur) {
-    const int kc0 = cur.k0 + CK * cur.ci;
-    constexpr int NBLK = CK / 16;
+    const int kc0 = cur.k0 + 32 * cur.ci;
     // K rows into the staging buffer and back in operand layout. Only this
     // wave touches its buffer and a wave's LDS accesses run in order; the
     // wave barrier keeps the compiler from moving the reads above the writes
     // (or the next chunk's writes above these reads).
 #pragma unroll
-    for (int b = 0; b < NBLK; ++b)
+    for (int b = 0; b < 2; ++b)
 #pragma unroll
-      for (int t = 0; t < KT; ++t) *reinterpret_cast<u32x4*>(kst + k_wr[t] + 16 * KROW * b) = c.k[b][t];
+      for (int t = 0; t < DC; ++t) *reinterpret_cast<u32x4*>(kst + k_wr[t] + 16 * KROW * b) = c.k[b][t];
     wave_lds_sync();
-    f32x4 s[NBLK];
+    f32x4 s[2];
 #pragma unroll
-    for (int b = 0; b < NBLK; ++b) {
+    for (int b = 0; b < 2; ++b) {
       s[b] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if constexpr (KV8) {
-        const float ks = scale_of(uint32_t(__builtin_amdgcn_readlane(int(c.scales), b)));
 #pragma unroll
-        for (int t = 0; t < KT; ++t) {
-          const u32x4 x = *reinterpret_cast<const u32x4*>(kst + k_rd[t] + 16 * KROW * b);
-          s[b] = mfma_16x16x32(codes_bf16x8(x[0], x[1], ks), qop[2 * t], s[b]);
-          s[b] = mfma_16x16x32(codes_bf16x8(x[2], x[3], ks), qop[2 * t + 1], s[b]);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-      } else {
-#pragma unroll
-        for (int cc = 0; cc < DC; ++cc)
-          s[b] = mfma_16x16x32(*reinterpret_cast<const u32x4*>(kst + k_rd[cc] + 16 * KROW * b), qop[cc], s[b]);
-      }
+      for (int cc = 0; cc < DC; ++cc)
+        s[b] = mfma_16x16x32(*reinterpret_cast<const u32x4*>(kst + k_rd[cc] + 16 * KROW * b), qop[cc], s[b]);
     }
     wave_lds_sync();
-    u32x4 pop[NBLK / 2];
-    softmax_chunk(s, kc0 + CK > cur.k1, kc0, cur.k1, gq, p.scale_log2, m, l, o, pop);
-    if constexpr (KV8) {
+    u32x4 pop[1];
+    softmax_chunk(s, kc0 + 32 > cur.k1, kc0, cur.k1, gq, p.scale_log2, m, l, o, pop);
+    u32x4 vop[DPL];
+    if constexpr (D == 128) transpose8x8(c.v, vop);
+    else transpose8x4(c.v, vop);
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {   // 32 keys: dword w of an operand holds keys 2w, 2w + 1 of the lane's 8
-        float vs[2];
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-          vs[b] = scale_of(uint32_t(__builtin_amdgcn_readlane(int(c.scales), 2 * h + b)) >> 8);
-#pragma unroll
-        for (int d = 0; d < DPL / 4; ++d) {   // 4 columns of the lane at a time
-          u32x4 vop[4];
-#pragma unroll
-          for (int w2 = 0; w2 < 4; ++w2) {
-            const auto& x = c.v[2 * h + (w2 >> 1)][2 * (w2 & 1)];
-            const auto& y = c.v[2 * h + (w2 >> 1)][2 * (w2 & 1) + 1];
-            uint32_t xd, yd;
-            if constexpr (D == 128) { xd = x[d]; yd = y[d]; }
-            else { xd = x; yd = y; }
-            const uint32_t lo = bytes_lo(xd, yd), hi = bytes_hi(xd, yd);
-            vop[0][w2] = codes_bf16x2<false>(lo, vs[w2 >> 1]);
-            vop[1][w2] = codes_bf16x2<true>(lo, vs[w2 >> 1]);
-            vop[2][w2] = codes_bf16x2<false>(hi, vs[w2 >> 1]);
-            vop[3][w2] = codes_bf16x2<true>(hi, vs[w2 >> 1]);
-          }
-#pragma unroll
-          for (int a = 0; a < 4; ++a) o[4 * d + a] = mfma_16x16x32(pop[h], vop[a], o[4 * d + a]);
-          __builtin_amdgcn_sched_barrier(0);
-        }
-      }
-    } else {
-      u32x4 vop[DPL];
-      if constexpr (D == 128) transpose8x8(c.v, vop);
-      else transpose8x4(c.v, vop);
-#pragma unroll
-      for (int a = 0; a < DPL; ++a) o[a] = mfma_16x16x32(pop[0], vop[a], o[a]);
-    }
+    for (int a = 0; a < DPL; ++a) o[a] = mfma_16x16x32(pop[0], vop[a], o[a]);
   };
 
   // Write piece i's result for this wave's head: the output of a whole
@@ -636,13 +462,13 @@ __device__ __forceinline__ void decode_gqa_body(const AttnParams& p, int range, 
   for (; fin < i_end; ++fin) finish(fin);
 }
 
-template <int D, int NW, int P, bool COMBINE, bool NT, bool KV8 = false>
+template <int D, int NW, int P, bool COMBINE, bool NT>
 __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 8)))
 void decode_gqa_kernel(AttnParams p) {
   // The waves' K staging buffers, then the range's block-table entries.
   extern __shared__ __attribute__((aligned(16))) uint8_t s_dyn[];
-  decode_gqa_body<D, NW, P, COMBINE, NT, KV8>(p, int(blockIdx.x), int(blockIdx.y), int(gridDim.y), int(threadIdx.x),
-                                              reinterpret_cast<int*>(s_dyn + NW * decode_kstage_bytes<D>()), s_dyn);
+  decode_gqa_body<D, NW, P, COMBINE, NT>(p, int(blockIdx.x), int(blockIdx.y), int(gridDim.y), int(threadIdx.x),
+                                         reinterpret_cast<int*>(s_dyn + NW * decode_kstage_bytes<D>()), s_dyn);
 }
 
 // ---------------------------------------------------------------------------
@@ -967,8 +793,8 @@ struct TileLoader8 {
 #pragma unroll
     for (int j = 0; j < NL; ++j) {
       const float f = scale_of(is_v[j] ? scale >> 8 : scale);
-      *reinterpret_cast<u32x4*>(stage + st_off[j][0]) = codes_bf16x8(x[j][0], x[j][1], f);
-      *reinterpret_cast<u32x4*>(stage + st_off[j][1]) = codes_bf16x8(x[j][2], x[j][3], f);
+      *reinterpret_cast<u32x4*>(stage + st_off[j][0]) = codes_bf16x8(x[j][0], x[j][1], f, f);
+      *reinterpret_cast<u32x4*>(stage + st_off[j][1]) = codes_bf16x8(x[j][2], x[j][3], f, f);
     }
   }
 };
@@ -1695,7 +1521,7 @@ static hipError_t launch_rowpar(const AttnParams& p, dim3 grid, hipStream_t stre
   return hipGetLastError();
 }
 
-template <int D, int P, bool KV8 = false>
+template <int D, int P>
 static hipError_t launch_decode_gqa(const AttnParams& p, hipStream_t stream) {
   // One work-group per (balanced range, KV head); the waves' K staging
   // buffers and the range's block-table entries take dynamic LDS.
@@ -1711,19 +1537,15 @@ static hipError_t launch_decode_gqa(const AttnParams& p, hipStream_t stream) {
     hipLaunchKernelGGL(kern, grid, dim3(nw * 64), lds, stream, p);
     return hipGetLastError();
   };
-  if (hw <= 2) return go(decode_gqa_kernel<D, 4, P, true, true, KV8>, 4);   // several waves per head, combined through LDS
-  if (hw <= 4) return go(decode_gqa_kernel<D, 4, P, false, true, KV8>, 4);
-  return go(decode_gqa_kernel<D, 8, P, false, true, KV8>, 8);
+  if (hw <= 2) return go(decode_gqa_kernel<D, 4, P, true, true>, 4);   // several waves per head, combined through LDS
+  if (hw <= 4) return go(decode_gqa_kernel<D, 4, P, false, true>, 4);
+  return go(decode_gqa_kernel<D, 8, P, false, true>, 8);
 }
 
 static hipError_t launch_decode_kernel(const AttnParams& p, int dqk, hipStream_t stream) {
   const bool p16 = p.P == 16;
   if (p.P != 16 && p.P != 64) return hipErrorInvalidValue;
-  if (p.kv_scales) {
-    if (dqk == 128) return p16 ? launch_decode_gqa<128, 16, true>(p, stream) : launch_decode_gqa<128, 64, true>(p, stream);
-    if (dqk == 64) return p16 ? launch_decode_gqa<64, 16, true>(p, stream) : launch_decode_gqa<64, 64, true>(p, stream);
-    return hipErrorInvalidValue;
-  }
+  if (p.kv_scales) return launch_decode_kv8(p, dqk, stream);
   const dim3 pieces(p.n_items, p.grid_y);
   switch (dqk) {
     case 128: return p16 ? launch_decode_gqa<128, 16>(p, stream) : launch_decode_gqa<128, 64>(p, stream);

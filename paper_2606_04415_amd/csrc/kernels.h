@@ -1,5 +1,5 @@
 // Kernel parameter blocks and launchers (host-callable, defined in attention.hip,
-// latent.hip and kv_append.hip).
+// decode_kv8.hip, latent.hip and kv_append.hip).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -51,6 +51,8 @@ inline hipError_t set_dynamic_lds(const void* kern, size_t bytes) {
 hipError_t launch_decode(const AttnParams& p, int head_dim_qk, bool has_splits, hipStream_t stream);
 // The split-K merge alone (after decode launches that skipped it).
 hipError_t launch_decode_merge(const AttnParams& p, int head_dim_qk, hipStream_t stream);
+// Grouped-query decode over an 8-bit cache, without the merge (decode_kv8.hip).
+hipError_t launch_decode_kv8(const AttnParams& p, int head_dim, hipStream_t stream);
 // Latent rows in groups of 128 (latent.hip).
 hipError_t launch_latent128(const AttnParams& p, bool decode, dim3 grid, hipStream_t stream);
 hipError_t launch_prefill(const AttnParams& p, int head_dim_qk, int bm, hipStream_t stream);

@@ -23,7 +23,8 @@ import sys
 from collections import defaultdict
 
 KERNEL_SOURCES = tuple(os.path.join(os.path.dirname(os.path.abspath(__file__)), "csrc", f)
-                       for f in ("attention.hip", "latent.hip", "latent_tile.h", "device_common.h"))
+                       for f in ("attention.hip", "decode_kv8.hip", "decode_walk.h", "latent.hip", "latent_tile.h",
+                                 "device_common.h"))
 COPY_BYTES = 1 << 30
 
 

@@ -214,6 +214,20 @@ def test_strided_cache():
     c.check(*out, "strided")
 
 
+@pytest.mark.parametrize("hq,hkv,d,P", [(28, 4, 128, 16), (10, 5, 64, 16), (8, 8, 64, 64), (4, 1, 64, 64)])
+def test_head_major_pages(hq, hkv, d, P):
+    """Pages laid out [head][slot][dim]: the rows behind a head's last key are
+    the next head's, and hold NaN in the last page."""
+    c = Case(hq, hkv, d, P, [1, 30, 1, 1], [100, 60, 500, 5], seed=hq)
+    g = c.gpu()
+    ref = c.run(g=g, min_split_tokens=64)
+    for n in "kv":
+        g[n] = g[n].view(torch.uint8).transpose(1, 2).contiguous().transpose(1, 2).view(torch.float8_e4m3fn)
+    out = c.run(g=g, min_split_tokens=64)
+    assert torch.equal(out[0].view(torch.int16), ref[0].view(torch.int16)) and torch.equal(out[1], ref[1])
+    c.check(*out, "head major")
+
+
 def test_captured_and_on_two_streams():
     c = Case(28, 4, 128, 16, [1, 1, 40], [3000, 500, 90], seed=10)
     ref = c.run(min_split_tokens=64)

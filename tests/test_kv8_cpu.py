@@ -263,7 +263,7 @@ def test_attention_refusals():
     for f, v in (("q", None), ("q", FAKE + 4), ("k_cache", FAKE + 8), ("v_cache", None), ("num_pages", 0), ("block_table_stride", 3),
                  ("k_stride", (ctypes.c_int64 * 3)(8192, 520, 128)), ("v_stride", (ctypes.c_int64 * 3)(8192, 512, 64)),
                  ("k_stride", (ctypes.c_int64 * 3)(1 << 31, 512, 128)), ("v_stride", (ctypes.c_int64 * 3)(8192, 1 << 27, 128)),
-                 ("workspace", None)):
+                 ("k_stride", (ctypes.c_int64 * 3)(8192, 512, 1 << 31)), ("workspace", None)):
         a = run_args(plan)
         setattr(a.attn, f, v)
         every(a)
