@@ -121,7 +121,7 @@ class Opts:
     cus_total: int = 0           # 0 -> 256
     cus_decode: int = 0          # 0 -> all; -1 -> cost model
     bm: int = 0                  # 0 -> 32 or 128 by batch size (128 for the latent layouts)
-    min_split_tokens: int = 0    # 0 -> 256
+    min_split_tokens: int = 0    # 0 -> 256 (64 with kv_bits 8)
     wg_per_cu: int = 0           # 0 -> 1 (grouped-query), 2 (576/512 latent layout)
     split_granule: int = 0       # 0 -> 32
     hbm_gbps: float = 0.0        # 0 -> 6500
@@ -174,7 +174,7 @@ def build_plan(sh: Shape, opts: Optional[Opts], qsl: Sequence[int], seq_lens: Se
     # --- option checks / defaults
     cus_total = o.cus_total or 256
     wg_per_cu = o.wg_per_cu or (2 if sh.head_dim_qk == 576 else 1)
-    min_tokens = o.min_split_tokens or 256
+    min_tokens = o.min_split_tokens or (64 if o.kv_bits == 8 else 256)
     granule = o.split_granule or 32
     mla = sh.head_dim_qk == 576
     split = sh.head_dim_qk == 192     # heads split out: prefill only, one tile per query head

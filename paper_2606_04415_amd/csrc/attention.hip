@@ -1566,6 +1566,9 @@ static hipError_t launch_decode_kernel(const AttnParams& p, int dqk, hipStream_t
 // together.
 static hipError_t launch_merge(const AttnParams& p, int dqk, hipStream_t stream) {
   if (p.n_merge == 0) return hipSuccess;
+  // Over an 8-bit cache, whose pieces are shorter: by rows when sequences have
+  // more than eight pieces in the mean, the one step of the merge by columns.
+  if (p.kv_scales && p.n_items > 8 * p.n_merge) return launch_merge_many(p, dqk, stream);
   const int dv = dqk == 576 ? 512 : dqk;
   const int units = p.rows_per_wg * (dv / 4);
   const dim3 mgrid(p.n_merge, p.grid_y, std::min(64, (units + 255) / 256));

@@ -214,6 +214,16 @@ def test_strided_cache():
     c.check(*out, "strided")
 
 
+@pytest.mark.parametrize("hq,hkv,d,P", [(28, 4, 128, 16), (20, 20, 64, 64), (24, 12, 128, 64), (4, 1, 64, 16)])
+def test_sequences_of_many_pieces(hq, hkv, d, P):
+    """More than eight pieces a sequence in the mean: merged a row at a time,
+    the rows of the heads that exist only (20 and 12 KV heads in columns of 8)."""
+    c = Case(hq, hkv, d, P, [1, 1, 1], [5000, 2999, 64], seed=hq)
+    pa = c.plan()
+    assert pa.plan.info["n_decode_items"] > 8 * pa.plan.info["n_split_seqs"]
+    c.check(*c.run("decode", pa=pa), "many pieces")
+
+
 @pytest.mark.parametrize("hq,hkv,d,P", [(28, 4, 128, 16), (10, 5, 64, 16), (8, 8, 64, 64), (4, 1, 64, 64)])
 def test_head_major_pages(hq, hkv, d, P):
     """Pages laid out [head][slot][dim]: the rows behind a head's last key are
