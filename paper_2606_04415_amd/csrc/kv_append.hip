@@ -66,26 +66,38 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendParams a) {
 // part apart, neighbouring pairs in one 32-byte piece; either way consecutive
 // threads read and write consecutive chunks.
 // ---------------------------------------------------------------------------
-// Positions of one token on its axes.
+// Positions of one token on its axes; ok: all inside the table (the others are
+// taken as 0, so that the table can be read before the token is given up).
+// AXES: more than one (kernels for one axis are a third of the code of those
+// for several, which costs short calls instruction fetches).
+template <bool AXES>
 struct Positions {
-  int32_t p[kRopeMaxAxes];
-  bool ok;
+  int32_t p[AXES ? kRopeMaxAxes : 1] = {};
+  bool ok = true;
 };
 
-__device__ __forceinline__ Positions read_positions(const RopeParams& r, int64_t t) {
-  Positions x;
-  x.ok = true;
+template <bool AXES>
+__device__ __forceinline__ void check_position(const RopeParams& r, Positions<AXES>& x, int a, int32_t pos) {
+  const bool ok = pos >= 0 && pos < r.max_position;
+  x.p[a] = ok ? pos : 0;
+  x.ok = x.ok && ok;
+}
+
+template <bool AXES>
+__device__ __forceinline__ Positions<AXES> read_positions(const RopeParams& r, int64_t t) {
+  Positions<AXES> x;
 #pragma unroll
-  for (int a = 0; a < kRopeMaxAxes; ++a) {
-    x.p[a] = a < r.n_axes ? r.positions[a * r.positions_stride + t] : 0;
-    x.ok = x.ok && x.p[a] >= 0 && x.p[a] < r.max_position;
-  }
+  for (int a = 0; a < (AXES ? kRopeMaxAxes : 1); ++a)
+    if (!AXES || a < r.n_axes) check_position(r, x, a, r.positions[a * r.positions_stride + t]);
   return x;
 }
 
-// The one position of a token that has no table of positions of its own.
-__device__ __forceinline__ Positions position_at(const RopeParams& r, int32_t pos) {
-  return Positions{{pos, 0, 0, 0}, pos >= 0 && pos < r.max_position};
+// The one position of a token that has no row of positions.
+template <bool AXES>
+__device__ __forceinline__ Positions<AXES> position_at(const RopeParams& r, int32_t pos) {
+  Positions<AXES> x;
+  check_position(r, x, 0, pos);
+  return x;
 }
 
 __device__ __forceinline__ int axis_of(const RopeParams& r, int i) {
@@ -98,34 +110,55 @@ __device__ __forceinline__ int axis_of(const RopeParams& r, int i) {
   return (r.n_axes > 1 && i >= s1 ? 1 : 0) + (r.n_axes > 2 && i >= s2 ? 1 : 0) + (r.n_axes > 3 && i >= s3 ? 1 : 0);
 }
 
-__device__ __forceinline__ int32_t pick(const Positions& x, int a) {
+__device__ __forceinline__ int32_t pick(const Positions<true>& x, int a) {
   return a == 0 ? x.p[0] : a == 1 ? x.p[1] : a == 2 ? x.p[2] : x.p[3];
 }
 
 // Cosines and sines of pairs 8 j .. 8 j + 7 at a token's positions: from one
-// table row when one axis has them all, else pair by pair.
+// table row when one axis has them all, from two when sections meet in the
+// unit, else pair by pair.
 struct Turn {
   float c[8], s[8];
 };
 
-__device__ __forceinline__ Turn read_turn(const RopeParams& r, const Positions& x, int j) {
+__device__ __forceinline__ Turn read_row(const RopeParams& r, int32_t pos, int j) {
+  const float* row = r.cos_sin + int64_t(pos) * r.rot_dim + 8 * j;
   Turn t;
-  const int half = r.rot_dim / 2;
-  const int a0 = r.n_axes == 1 ? 0 : axis_of(r, 8 * j);
-  if (r.n_axes == 1 || (!r.dealt && axis_of(r, 8 * j + 7) == a0)) {
-    const float* row = r.cos_sin + int64_t(pick(x, a0)) * r.rot_dim + 8 * j;
 #pragma unroll
-    for (int v = 0; v < 2; ++v) {
-      const f32x4 c = *reinterpret_cast<const f32x4*>(row + 4 * v);
-      const f32x4 s = *reinterpret_cast<const f32x4*>(row + half + 4 * v);
+  for (int v = 0; v < 2; ++v) {
+    const f32x4 c = *reinterpret_cast<const f32x4*>(row + 4 * v);
+    const f32x4 s = *reinterpret_cast<const f32x4*>(row + r.rot_dim / 2 + 4 * v);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        t.c[4 * v + e] = c[e];
-        t.s[4 * v + e] = s[e];
-      }
+    for (int e = 0; e < 4; ++e) {
+      t.c[4 * v + e] = c[e];
+      t.s[4 * v + e] = s[e];
     }
-    return t;
   }
+  return t;
+}
+
+__device__ __forceinline__ Turn read_turn(const RopeParams& r, const Positions<false>& x, int j) {
+  return read_row(r, x.p[0], j);
+}
+__device__ __forceinline__ Turn read_turn(const RopeParams& r, const Positions<true>& x, int j) {
+  const int half = r.rot_dim / 2;
+  if (!r.dealt) {
+    const int a0 = axis_of(r, 8 * j), a1 = axis_of(r, 8 * j + 7);
+    if (a1 <= a0 + 1) {
+      Turn t = read_row(r, pick(x, a0), j);
+      if (a1 != a0) {
+        const Turn u = read_row(r, pick(x, a1), j);
+#pragma unroll
+        for (int e = 1; e < 8; ++e) {
+          const bool next = axis_of(r, 8 * j + e) != a0;
+          t.c[e] = next ? u.c[e] : t.c[e];
+          t.s[e] = next ? u.s[e] : t.s[e];
+        }
+      }
+      return t;
+    }
+  }
+  Turn t;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const float* row = r.cos_sin + int64_t(pick(x, axis_of(r, 8 * j + e))) * r.rot_dim + 8 * j + e;
@@ -183,95 +216,128 @@ __device__ __forceinline__ void turn_unit(const RopeParams& r, const Turn& t, fl
   }
 }
 
-// One unit of a head's row from src to dst (both at the head's first column).
-__device__ __forceinline__ void move_unit(const RopeParams& r, const Positions& x, int j, const uint16_t* src,
-                                          uint16_t* dst) {
+// Heads that one thread takes: it reads the cosines and sines of its unit once
+// for all of them, and their loads are in flight together. (One head a thread,
+// 2176 tokens of 28/4 heads of 128: 12.3 us against MEASURED_ROPE_MIXED; tokens on three axes
+// whose units have pairs of two of them: 25.4 against MEASURED_ROPE_AXES.)
+constexpr int kHeadsPerThread = 4;
+
+// Unit j of heads h .. h + kHeadsPerThread - 1 of a token's n_heads rows, from
+// src(head) to dst(head) (a row's first column), written if live(); heads past
+// the last repeat it and are not written.
+template <bool AXES, typename Live, typename Src, typename Dst>
+__device__ __forceinline__ void move_units(const RopeParams& r, const Positions<AXES>& x, int j, int h, int n_heads, Live&& live,
+                                           Src&& src, Dst&& dst) {
   int c0, c1;
   unit_columns(r, j, c0, c1);
-  u32x4 v0 = load16(src + c0), v1 = load16(src + c1);
+  u32x4 v0[kHeadsPerThread], v1[kHeadsPerThread];
+#pragma unroll
+  for (int k = 0; k < kHeadsPerThread; ++k) {
+    const uint16_t* s = src(min(h + k, n_heads - 1));
+    v0[k] = load16(s + c0);
+    v1[k] = load16(s + c1);
+  }
   if (j < r.rot_dim / 16) {
     const Turn t = read_turn(r, x, j);
-    float a[8], b[8];
-    unpack8(v0, a);
-    unpack8(v1, b);
-    turn_unit(r, t, a, b);
-    v0 = pack8(a);
-    v1 = pack8(b);
+#pragma unroll
+    for (int k = 0; k < kHeadsPerThread; ++k) {
+      float a[8], b[8];
+      unpack8(v0[k], a);
+      unpack8(v1[k], b);
+      turn_unit(r, t, a, b);
+      v0[k] = pack8(a);
+      v1[k] = pack8(b);
+    }
   }
-  *reinterpret_cast<u32x4*>(dst + c0) = v0;
-  *reinterpret_cast<u32x4*>(dst + c1) = v1;
+  if (!live()) return;
+#pragma unroll
+  for (int k = 0; k < kHeadsPerThread; ++k) {
+    if (h + k >= n_heads) break;
+    uint16_t* d = dst(h + k);
+    *reinterpret_cast<u32x4*>(d + c0) = v0[k];
+    *reinterpret_cast<u32x4*>(d + c1) = v1[k];
+  }
 }
 
 // ---------------------------------------------------------------------------
-// Into the bf16 cache: a work-group takes `per_wg` tokens and walks their
-// units (queries, keys, values). Bound by HBM; the table rows are read by every
-// head of a token and come from the caches.
+// Into the bf16 cache: a work-group takes `per_wg` tokens; a thread takes one
+// unit of four consecutive heads (queries, then keys), or 32 bytes of values.
+// Bound by HBM.
 // ---------------------------------------------------------------------------
-template <int DK, int DV>
+template <int DK, int DV, bool AXES>
 __global__ __launch_bounds__(512) void rope_append_kernel(RopeAppendParams p) {
   constexpr int UK = DK / 16, UV = DV / 16;
   const AppendParams& a = p.kv;
-  const int nq = p.Hq * UK, nk = p.Hkv * UK, nv = a.cv ? p.Hkv * UV : 0;
-  const int per_tok = nq + nk + nv;
+  const int heads = p.Hq + p.Hkv;
+  const int nqk = (heads + kHeadsPerThread - 1) / kHeadsPerThread * UK, nv = a.cv ? p.Hkv * UV : 0;
+  const int per_tok = nqk + nv, page_bits = __builtin_ctz(a.P);   // (pages of 16 or 64)
   const int64_t t0 = int64_t(blockIdx.x) * p.per_wg;
   const int n = int(min(int64_t(p.per_wg), a.n_tokens - t0)) * per_tok;
   for (int i = threadIdx.x; i < n; i += blockDim.x) {
     const int dt = p.per_wg == 1 ? 0 : i / per_tok;
-    int u = i - dt * per_tok;
+    const int u = i - dt * per_tok;
     const int64_t t = t0 + dt;
     const int32_t slot = a.slot_mapping[t];
-    if (slot < 0) continue;                    // padding token
-    const Positions x = read_positions(p.rope, t);
-    if (!x.ok || int64_t(slot) >= a.num_slots) {
-      if (u == 0 && a.bad_count) atomicAdd(a.bad_count, 1);
-      continue;
-    }
-    if (u < nq) {
-      const int h = u / UK;
-      move_unit(p.rope, x, u - h * UK, p.q + t * p.q_stride + h * DK, p.q_out + (t * p.Hq + h) * DK);
-      continue;
-    }
-    u -= nq;
-    const int64_t page = slot / a.P, row = slot - page * a.P;
-    if (u < nk) {
-      const int h = u / UK;
-      move_unit(p.rope, x, u - h * UK, a.k_new + t * a.k_new_stride + h * DK,
-                const_cast<uint16_t*>(a.kc.base) + page * a.kc.sp + row * a.kc.ss + h * a.kc.sh);
+    const auto x = read_positions<AXES>(p.rope, t);
+    // A negative slot is padding; another fault is counted once a token.
+    const bool inside = slot >= 0 && int64_t(slot) < a.num_slots, live = inside && x.ok;
+    const int64_t page = inside ? slot >> page_bits : 0, row = inside ? slot & (a.P - 1) : 0;
+    if (u < nqk) {
+      const int g = u / UK;
+      move_units(
+          p.rope, x, u - g * UK, g * kHeadsPerThread, heads, [&] { return live; },
+          [&](int h) { return h < p.Hq ? p.q + t * p.q_stride + h * DK : a.k_new + t * a.k_new_stride + (h - p.Hq) * DK; },
+          [&](int h) {
+            return h < p.Hq ? p.q_out + (t * p.Hq + h) * DK
+                            : const_cast<uint16_t*>(a.kc.base) + page * a.kc.sp + row * a.kc.ss + (h - p.Hq) * a.kc.sh;
+          });
     } else {
-      u -= nk;
-      const int h = u / UV, c = 16 * (u - h * UV);
+      const int v = u - nqk, h = v / UV, c = 16 * (v - h * UV);
       const uint16_t* src = a.v_new + t * a.v_new_stride + h * DV + c;
-      uint16_t* dst = const_cast<uint16_t*>(a.vc.base) + page * a.vc.sp + row * a.vc.ss + h * a.vc.sh + c;
       const u32x4 v0 = load16(src), v1 = load16(src + 8);
+      if (!live) continue;   // (never a token's unit 0)
+      uint16_t* dst = const_cast<uint16_t*>(a.vc.base) + page * a.vc.sp + row * a.vc.ss + h * a.vc.sh + c;
       *reinterpret_cast<u32x4*>(dst) = v0;
       *reinterpret_cast<u32x4*>(dst + 8) = v1;
     }
+    if (u == 0 && slot >= 0 && !live && a.bad_count) atomicAdd(a.bad_count, 1);
   }
 }
 
 // ---------------------------------------------------------------------------
 // Into the 8-bit cache. Work-group t takes new token t: it finds the token's
-// sequence, turns its query, and, when the token is the first of its block in
-// this call, quantises the block's new rows, one wave for each KV head and K or
-// V (the rows of a block are consecutive new tokens, so no two work-groups
-// touch a block). A wave holds its rows in registers between the maximum that
-// gives the scale and the conversion, so they are read once.
+// sequence, turns its query, and takes its part of the token's block: a task is
+// the block's new rows of one KV head, K or V, for one wave, and the
+// work-groups of the block's new tokens (which are consecutive) share them out.
+// A wave holds its rows in registers between the maximum that gives the scale
+// and the conversion, so they are read once. (With all tasks of a block in the
+// work-group of its first token, a 2048-token chunk beside 128 decodes took
+// 33.6 us, now MEASURED_KV8_MIXED.)
 // ---------------------------------------------------------------------------
 
-// The sequence that holds new token t (B: none): the largest s with
-// query_start_loc[s] <= t, 64 probes at a time.
-__device__ __forceinline__ int find_sequence(const int32_t* qsl, int B, int64_t t, int lane) {
-  int base = 0, len = B;
-  while (len > 0) {
-    const int step = (len + 63) / 64;
-    const int64_t x = base + int64_t(lane + 1) * step;
-    const bool below = x <= base + len && int64_t(qsl[x]) <= t;
+// The sequence that holds new token t: the largest s with query_start_loc[s]
+// <= t (B: none, padding), its first and end token and its length. 63 probes at
+// a time; the last round, over 64 neighbours, brings the rest along.
+struct Sequence {
+  int s, start, end, L;
+};
+
+__device__ __forceinline__ Sequence find_sequence(const int32_t* qsl, const int32_t* seq_lens, int B, int64_t t, int lane) {
+  int base = 0, len = B;                 // s lies in base .. base + len
+  while (len > 62) {
+    const int step = (len + 62) / 63;
+    const int64_t at = base + int64_t(lane + 1) * step;
+    const bool below = lane < 63 && at <= base + len && int64_t(qsl[min(at, int64_t(B))]) <= t;
     const int n = __popcll(__builtin_amdgcn_ballot_w64(below));
     const int end = base + len;
     base += n * step;
     len = min(step - 1, end - base);
   }
-  return __builtin_amdgcn_readfirstlane(base);
+  const int v = qsl[min(base + lane, B)], held = seq_lens[min(base + lane, B - 1)];
+  const bool below = lane > 0 && lane <= len && int64_t(v) <= t;
+  const int n = __popcll(__builtin_amdgcn_ballot_w64(below));
+  return Sequence{__builtin_amdgcn_readfirstlane(base + n), __builtin_amdgcn_readlane(v, n),
+                  __builtin_amdgcn_readlane(v, n + 1), __builtin_amdgcn_readlane(held, n)};
 }
 
 // Least k >= -117 with a <= 448 * 2^k, from the bits of a >= 0. 448 = 1.75 *
@@ -298,126 +364,179 @@ __device__ __forceinline__ uint32_t rescale4(uint32_t c, float f) {
   return encode4(lo[0] * f, lo[1] * f, hi[0] * f, hi[1] * f);
 }
 
+// Maximum over the wave: rotations within rows of 16 lanes, then swaps of rows.
+template <int N>
+__device__ __forceinline__ uint32_t row_ror(uint32_t v) {
+  return uint32_t(__builtin_amdgcn_update_dpp(0, int(v), 0x120 + N, 0xF, 0xF, false));
+}
 __device__ __forceinline__ uint32_t wave_max(uint32_t v) {
-#pragma unroll
-  for (int m = 1; m < 64; m *= 2) v = max(v, uint32_t(__shfl_xor(int(v), m, 64)));
-  return v;
+  v = max(v, row_ror<8>(v));
+  v = max(v, row_ror<4>(v));
+  v = max(v, row_ror<2>(v));
+  v = max(v, row_ror<1>(v));
+  const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = max(a[0], a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return uint32_t(__builtin_amdgcn_readfirstlane(int(max(b[0], b[1]))));
 }
 
-// Rows r0 .. r1 - 1 of one block for one KV head, keys or values: row r is new
-// token t + r - r0. codes: the block's row 0 at this head; scale: its byte.
-template <int D>
-__device__ __forceinline__ void quantise_block(const Kv8AppendParams& p, bool turn, const uint16_t* src, int64_t stride,
-                                               int64_t t, int32_t pos, int r0, int r1, uint8_t* codes, int64_t ss,
-                                               uint8_t* scale, int lane) {
-  constexpr int U = D / 16;              // units of a row
-  constexpr int RPP = 64 / U;            // rows of a pass
-  constexpr int PASSES = 16 / RPP;
-  const RopeParams& r = p.rope;
-  const bool kept = r0 > 0;              // the block holds earlier rows of the sequence
-  const int old = kept ? int(*scale) - 127 : -128;
-  const int j = lane % U;
-  int c0 = 16 * j, c1 = c0 + 8;
-  if (turn) unit_columns(r, j, c0, c1);
-  float a[PASSES][8], b[PASSES][8];
-  bool write[PASSES];
-  uint32_t top = 0;
-#pragma unroll
-  for (int i = 0; i < PASSES; ++i) {
-    const int row = i * RPP + lane / U;
-    write[i] = row >= r0 && row < r1;
-    if (!write[i]) continue;
-    const int64_t tok = t + row - r0;
-    Positions x{{0, 0, 0, 0}, true};
-    if (r.cos_sin) x = r.positions ? read_positions(r, tok) : position_at(r, pos + row - r0);
-    if (!x.ok) {
-      write[i] = false;
-      continue;
-    }
-    unpack8(load16(src + tok * stride + c0), a[i]);
-    unpack8(load16(src + tok * stride + c1), b[i]);
-    if (turn && j < r.rot_dim / 16) turn_unit(r, read_turn(r, x, j), a[i], b[i]);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const uint32_t ua = __float_as_uint(a[i][e]) & 0x7FFFFFFFu, ub = __float_as_uint(b[i][e]) & 0x7FFFFFFFu;
-      top = max(top, max(ua < 0x7F800000u ? ua : 0u, ub < 0x7F800000u ? ub : 0u));
-    }
-  }
-  const int k = max(scale_exponent(wave_max(top)), old);
-  if (kept && k > old) {   // a power of two: codes stay exact down to the subnormal ones
-    const float f = power_of_two(old - k);
-    for (int i = lane; i < r0 * U; i += 64) {
-      u32x4* at = reinterpret_cast<u32x4*>(codes + (i / U) * ss + 16 * (i % U));
-      u32x4 v = *at;
-#pragma unroll
-      for (int w = 0; w < 4; ++w) v[w] = rescale4(v[w], f);
-      *at = v;
-    }
-  }
-  const float inv = __uint_as_float(uint32_t(max(127 - k, 1)) << 23);
-#pragma unroll
-  for (int i = 0; i < PASSES; ++i) {
-    if (!write[i]) continue;
-    uint8_t* row = codes + (i * RPP + lane / U) * ss;
-    const auto code = [&](const float (&x)[8]) {
-      return u32x2{encode4(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv),
-                   encode4(x[4] * inv, x[5] * inv, x[6] * inv, x[7] * inv)};
-    };
-    *reinterpret_cast<u32x2*>(row + c0) = code(a[i]);
-    *reinterpret_cast<u32x2*>(row + c1) = code(b[i]);
-  }
-  if (lane == 0) *scale = uint8_t(k + 127);
-}
+// The `count` new rows of one block for one KV head, keys or values, in a wave's
+// registers: those of new tokens t, t + 1, ... Lane l holds unit l % U of row
+// l / U of each pass. All loads are issued before the first value is used, lanes
+// past the last row reading it again.
+template <int D, int PASSES, bool AXES>
+struct Block {
+  static constexpr int U = D / 16;              // units of a row
+  static constexpr int RPP = 64 / U;            // rows of a pass
+  int c0, c1;
+  float a[PASSES][8], b[PASSES][8];             // a unit's two chunks
+  bool mine[PASSES];                            // the lane has a row to write
 
-template <int D>
+  __device__ __forceinline__ void read(const Kv8AppendParams& p, bool turn, const uint16_t* src, int64_t stride, int64_t t,
+                                       int32_t pos, int count, int lane) {
+    const RopeParams& r = p.rope;
+    const int j = lane % U;
+    c0 = 16 * j;
+    c1 = c0 + 8;
+    if (turn) unit_columns(r, j, c0, c1);
+    u32x4 v0[PASSES], v1[PASSES];
+    Positions<AXES> x[PASSES];
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i) {
+      const int at = min(i * RPP + lane / U, count - 1);
+      v0[i] = load16(src + (t + at) * stride + c0);
+      v1[i] = load16(src + (t + at) * stride + c1);
+      if (r.cos_sin) x[i] = r.positions ? read_positions<AXES>(r, t + at) : position_at<AXES>(r, pos + at);
+      mine[i] = at == i * RPP + lane / U && x[i].ok;
+    }
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i) {
+      unpack8(v0[i], a[i]);
+      unpack8(v1[i], b[i]);
+      if (turn && j < r.rot_dim / 16) turn_unit(r, read_turn(r, x[i], j), a[i], b[i]);
+    }
+  }
+
+  // codes: the block's row 0 at this head, ss bytes from row to row; scale: its
+  // byte. The new rows are r0, r0 + 1, ..; earlier rows of the sequence are
+  // there iff r0 > 0.
+  __device__ __forceinline__ void write(uint8_t* codes, int64_t ss, uint8_t* scale, int r0, int lane) const {
+    const int old = r0 > 0 ? int(*scale) - 127 : -128;
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i) {
+      uint32_t most = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t ua = __float_as_uint(a[i][e]) & 0x7FFFFFFFu, ub = __float_as_uint(b[i][e]) & 0x7FFFFFFFu;
+        most = max(most, max(ua < 0x7F800000u ? ua : 0u, ub < 0x7F800000u ? ub : 0u));
+      }
+      top = max(top, mine[i] ? most : 0u);
+    }
+    const int k = max(scale_exponent(wave_max(top)), old);
+    if (r0 > 0 && k > old) {   // a power of two: codes stay exact down to the subnormal ones
+      const float f = power_of_two(old - k);
+      for (int i = lane; i < r0 * U; i += 64) {
+        u32x4* at = reinterpret_cast<u32x4*>(codes + (i / U) * ss + 16 * (i % U));
+        u32x4 v = *at;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) v[w] = rescale4(v[w], f);
+        *at = v;
+      }
+    }
+    const float inv = __uint_as_float(uint32_t(max(127 - k, 1)) << 23);
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i) {
+      if (!mine[i]) continue;
+      uint8_t* row = codes + (r0 + i * RPP + lane / U) * ss;
+      const auto code = [&](const float (&y)[8]) {
+        return u32x2{encode4(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv),
+                     encode4(y[4] * inv, y[5] * inv, y[6] * inv, y[7] * inv)};
+      };
+      *reinterpret_cast<u32x2*>(row + c0) = code(a[i]);
+      *reinterpret_cast<u32x2*>(row + c1) = code(b[i]);
+    }
+    if (lane == 0) *scale = uint8_t(k + 127);
+  }
+};
+
+template <int D, bool AXES>
 __global__ __launch_bounds__(256) void kv8_append_kernel(Kv8AppendParams p) {
   constexpr int U = D / 16;
   const int64_t t = blockIdx.x;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int s = find_sequence(p.qsl, p.num_seqs, t, lane);
-  if (s >= p.num_seqs) return;           // padding token
-  const int64_t q0 = p.qsl[s], q1 = min(int64_t(p.qsl[s + 1]), p.n_tokens);
-  const int32_t pos = int32_t(p.seq_lens[s] - (p.qsl[s + 1] - t));
-  const int32_t page_at = pos / p.P;
-  int32_t page = -1;
-  if (pos >= 0 && page_at < p.bt_stride) page = p.bt[int64_t(s) * p.bt_stride + page_at];
-  const bool paged = page >= 0 && int64_t(page) < p.num_pages;
   const bool rope = p.rope.cos_sin != nullptr;
-  Positions x{{0, 0, 0, 0}, true};
-  if (rope) x = p.rope.positions ? read_positions(p.rope, t) : position_at(p.rope, pos);
-  if (!paged || !x.ok) {
-    if (threadIdx.x == 0 && p.bad_count) atomicAdd(p.bad_count, 1);
-  } else if (rope) {
-    for (int u = threadIdx.x; u < p.Hq * U; u += blockDim.x) {
-      const int h = u / U;
-      move_unit(p.rope, x, u - h * U, p.q + t * p.q_stride + h * D, p.q_out + (t * p.Hq + h) * D);
+  Positions<AXES> x;
+  if (rope && p.rope.positions) x = read_positions<AXES>(p.rope, t);
+  const Sequence q = find_sequence(p.qsl, p.seq_lens, p.num_seqs, t, lane);
+  if (q.s >= p.num_seqs) return;         // padding token
+  const int64_t q1 = min(int64_t(q.end), p.n_tokens);
+  const int32_t pos = int32_t(q.L - (q.end - t));
+  if (rope && !p.rope.positions) x = position_at<AXES>(p.rope, pos);
+  // The page is loaded here and waited for where something is written: rows,
+  // positions and table come in the meantime.
+  const int32_t page_at = pos >> __builtin_ctz(p.P);
+  const bool in_row = pos >= 0 && page_at < p.bt_stride;
+  const int32_t page = p.bt[int64_t(q.s) * p.bt_stride + (in_row ? page_at : 0)];
+  if (rope) {
+    for (int u = threadIdx.x; u < (p.Hq + kHeadsPerThread - 1) / kHeadsPerThread * U; u += blockDim.x) {
+      const int g = u / U;
+      move_units(
+          p.rope, x, u - g * U, g * kHeadsPerThread, p.Hq, [&] { return x.ok && in_row && page >= 0 && page < p.num_pages; },
+          [&](int h) { return p.q + t * p.q_stride + h * D; }, [&](int h) { return p.q_out + (t * p.Hq + h) * D; });
     }
   }
-  const int r0 = pos & 15;
-  if (!paged || (t != q0 && r0 != 0)) return;   // the block is an earlier token's
-  const int r1 = int(min(int64_t(16), r0 + (q1 - t)));
-  const int64_t row0 = pos % p.P - r0;          // the block's first slot in its page
-  for (int task = w; task < 2 * p.Hkv; task += blockDim.x / 64) {
-    const int kv = task & 1, h = task >> 1;
-    uint8_t* codes = kv ? p.v + page * p.v_sp + row0 * p.v_ss + h * p.v_sh : p.k + page * p.k_sp + row0 * p.k_ss + h * p.k_sh;
-    uint8_t* scale = p.scales + page * p.scale_sp + (row0 / 16 * p.Hkv + h) * 2 + kv;
-    quantise_block<D>(p, rope && !kv, (kv ? p.v_new : p.k_new) + h * D, kv ? p.v_new_stride : p.k_new_stride, t, pos, r0,
-                      r1, codes, kv ? p.v_ss : p.k_ss, scale, lane);
+  // The token's block holds `count` of the call's new rows, from row r0 on, and
+  // this token's is the `rank`-th: its work-group takes every count-th task (a
+  // KV head, or its K or V), from the last wave down (the first ones turn
+  // queries).
+  const int32_t first = max(pos & ~15, q.L - (q.end - max(q.start, 0)));   // position of the block's first new row
+  const int r0 = first & 15, rank = pos - first;
+  const int64_t tf = t - rank;
+  const int count = int(min(int64_t(16 - r0), q1 - tf));
+  const int64_t row0 = pos & (p.P - 1) & ~15;         // the block's first slot in its page
+  const auto read = [&](auto& b, int h, int kv) {
+    b.read(p, rope && !kv, (kv ? p.v_new : p.k_new) + h * D, kv ? p.v_new_stride : p.k_new_stride, tf, first, count, lane);
+  };
+  const auto write = [&](const auto& b, int h, int kv) {
+    b.write(kv ? p.v + page * p.v_sp + row0 * p.v_ss + h * p.v_sh : p.k + page * p.k_sp + row0 * p.k_ss + h * p.k_sh,
+            kv ? p.v_ss : p.k_ss, p.scales + page * p.scale_sp + (row0 / 16 * p.Hkv + h) * 2 + kv, r0, lane);
+  };
+  const auto paged = [&] { return in_row && page >= 0 && page < p.num_pages; };
+  const int waves = blockDim.x / 64, mine = rank + (waves - 1 - w) * count;
+  constexpr int RPP = 64 / U;
+  if (count <= RPP) {          // one pass holds the rows: keys and values of a head side by side
+    for (int h = mine; h < p.Hkv; h += waves * count) {
+      Block<D, 1, AXES> k, v;
+      read(k, h, 0);
+      read(v, h, 1);
+      if (!paged()) break;
+      write(k, h, 0);
+      write(v, h, 1);
+    }
+  } else {
+    for (int task = mine; task < 2 * p.Hkv; task += waves * count) {
+      Block<D, 16 / RPP, AXES> b;
+      read(b, task >> 1, task & 1);
+      if (!paged()) break;
+      write(b, task >> 1, task & 1);
+    }
   }
+  if (threadIdx.x == 0 && !(x.ok && paged()) && p.bad_count) atomicAdd(p.bad_count, 1);
 }
 
-template <int DK, int DV>
+template <int DK, int DV, bool AXES>
 hipError_t launch_rope_append_t(RopeAppendParams p, hipStream_t stream) {
   // Work-groups of up to 512 threads: a token's units, or those of as many
   // tokens as 512 threads cover at one unit each; when a token has more, as
   // few threads as take them in the same number of rounds.
-  const int units = (p.Hq + p.Hkv) * (DK / 16) + (p.kv.cv ? p.Hkv * (DV / 16) : 0);
+  const int units = (p.Hq + p.Hkv + kHeadsPerThread - 1) / kHeadsPerThread * (DK / 16) + (p.kv.cv ? p.Hkv * (DV / 16) : 0);
   p.per_wg = int32_t(std::min<int64_t>(std::max(1, 512 / units), p.kv.n_tokens));
   const int n = units * p.per_wg, rounds = (n + 511) / 512;
   const int threads = ((n + rounds - 1) / rounds + 63) / 64 * 64;
   const int64_t blocks = (p.kv.n_tokens + p.per_wg - 1) / p.per_wg;
   if (blocks > INT32_MAX) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((rope_append_kernel<DK, DV>), dim3(uint32_t(blocks)), dim3(threads), 0, stream, p);
+  hipLaunchKernelGGL((rope_append_kernel<DK, DV, AXES>), dim3(uint32_t(blocks)), dim3(threads), 0, stream, p);
   return hipGetLastError();
 }
 
@@ -434,11 +553,12 @@ hipError_t launch_kv_append(const AppendParams& a, hipStream_t stream) {
 
 hipError_t launch_rope_append(const RopeAppendParams& p, hipStream_t stream) {
   if (p.kv.n_tokens == 0) return hipSuccess;
+  const bool axes = p.rope.n_axes > 1;
   switch (p.kv.dk) {
-    case 64: return launch_rope_append_t<64, 64>(p, stream);
-    case 128: return launch_rope_append_t<128, 128>(p, stream);
-    case 192: return launch_rope_append_t<192, 128>(p, stream);
-    case 576: return launch_rope_append_t<576, 512>(p, stream);
+    case 64: return axes ? launch_rope_append_t<64, 64, true>(p, stream) : launch_rope_append_t<64, 64, false>(p, stream);
+    case 128: return axes ? launch_rope_append_t<128, 128, true>(p, stream) : launch_rope_append_t<128, 128, false>(p, stream);
+    case 192: return axes ? launch_rope_append_t<192, 128, true>(p, stream) : launch_rope_append_t<192, 128, false>(p, stream);
+    case 576: return axes ? launch_rope_append_t<576, 512, true>(p, stream) : launch_rope_append_t<576, 512, false>(p, stream);
     default: return hipErrorInvalidValue;
   }
 }
@@ -446,10 +566,11 @@ hipError_t launch_rope_append(const RopeAppendParams& p, hipStream_t stream) {
 hipError_t launch_kv8_append(const Kv8AppendParams& p, int head_dim, hipStream_t stream) {
   if (p.n_tokens == 0 || p.num_seqs == 0) return hipSuccess;
   if (p.n_tokens > INT32_MAX) return hipErrorInvalidValue;
-  const dim3 grid(uint32_t(p.n_tokens)), threads(256);
-  if (head_dim == 128) hipLaunchKernelGGL(kv8_append_kernel<128>, grid, threads, 0, stream, p);
-  else if (head_dim == 64) hipLaunchKernelGGL(kv8_append_kernel<64>, grid, threads, 0, stream, p);
-  else return hipErrorInvalidValue;
+  if (head_dim != 64 && head_dim != 128) return hipErrorInvalidValue;
+  const bool axes = p.rope.n_axes > 1;
+  const auto kern = head_dim == 128 ? (axes ? kv8_append_kernel<128, true> : kv8_append_kernel<128, false>)
+                                    : (axes ? kv8_append_kernel<64, true> : kv8_append_kernel<64, false>);
+  hipLaunchKernelGGL(kern, dim3(uint32_t(p.n_tokens)), dim3(256), 0, stream, p);
   return hipGetLastError();
 }
 

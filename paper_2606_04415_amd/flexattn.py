@@ -491,14 +491,20 @@ def _one_device(tensors):
     return devs.pop()
 
 
-def _run(what, args, stream, *call):
-    """Calls lib().<what>(*call, stream) on the device of args' tensors, on its
+def _run(what, args, stream, *call, last=()):
+    """Calls lib().<what>(*call, stream, *last) on the device of args' tensors, on its
     current stream unless one is given. ValueError for tensors that are not on a GPU."""
     import torch
-    _require(args.device.type == "cuda", f"{what} needs GPU tensors, not {args.device}")
-    with torch.cuda.device(args.device):
-        s = stream if stream is not None else current_stream()
-        check(getattr(lib(), what)(*call, s), what)
+    dev = args.device
+    if dev.type != "cuda":
+        raise ValueError(f"{what} needs GPU tensors, not {dev}")
+    if dev.index == torch.cuda.current_device():
+        st = getattr(lib(), what)(*call, stream if stream is not None else current_stream(), *last)
+    else:
+        with torch.cuda.device(dev):
+            st = getattr(lib(), what)(*call, stream if stream is not None else current_stream(), *last)
+    if st != FLEX_OK:
+        check(st, what)
 
 
 def _rows(name, t, heads, dim, dtype=None):
@@ -566,9 +572,10 @@ def make_rope(cos_sin, positions=None, rot_begin: int = 0, neighbours: bool = Fa
 
 
 def _check_rope(rope, args, n_tokens):
-    _require(rope.device == args.device, f"rope on {rope.device}, tensors on {args.device}")
-    _require(rope.n_positions is None or rope.n_positions >= n_tokens,
-             f"{rope.n_positions} positions for {n_tokens} tokens")
+    if rope.device != args.device:
+        raise ValueError(f"rope on {rope.device}, tensors on {args.device}")
+    if rope.n_positions is not None and rope.n_positions < n_tokens:
+        raise ValueError(f"{rope.n_positions} positions for {n_tokens} tokens")
 
 
 def make_rope_append_args(q, q_out, k_new, v_new, slot_mapping, k_cache, v_cache, bad_count=None) -> RopeAppendArgs:
@@ -599,12 +606,11 @@ def make_rope_append_args(q, q_out, k_new, v_new, slot_mapping, k_cache, v_cache
 
 
 def _check_sizes(shape, args):
-    want = (shape.num_q_heads, shape.num_kv_heads, shape.head_dim_qk, None if shape.v_aliases_k else shape.head_dim_v,
-            shape.page_size)
-    _require(all(b is _ANY or a == b for a, b in zip(want, args.sizes)), f"tensors for {args.sizes}, shape {want}")
-
-
-_ANY = object()
+    """args.sizes: query heads (None: no queries), KV heads, key and value width (None: aliased), page size."""
+    hq, *rest = args.sizes
+    want = [shape.num_kv_heads, shape.head_dim_qk, None if shape.v_aliases_k else shape.head_dim_v, shape.page_size]
+    if rest != want or (hq is not None and hq != shape.num_q_heads):
+        raise ValueError(f"tensors for {args.sizes}, shape {(shape.num_q_heads, *want)}")
 
 
 def flex_attn_rope_append(shape: Shape, rope: Rope, args: RopeAppendArgs, stream=None):
@@ -651,7 +657,7 @@ def make_kv8_append_args(k_new, v_new, block_table, seq_lens, query_start_loc, k
     a.v_new, a.v_new_stride = v_new.data_ptr(), _rows("v_new", v_new, heads, d)
     _require(v_new.shape[0] == n, "k_new and v_new must have the same tokens")
     _require((q is None) == (q_out is None), "q and q_out are given together")
-    Hq = _ANY
+    Hq = None
     if q is not None:
         Hq = q.shape[1]
         a.q, a.q_stride, a.q_out = q.data_ptr(), _rows("q", q, Hq, d), q_out.data_ptr()
@@ -705,12 +711,8 @@ def flex_attn_prefill_kv8(plan: Plan, args: Kv8Args, stream=None):
 
 
 def flex_attn_mixed_kv8(plan: Plan, args: Kv8Args, mode: int, stream=None, corun: "Corun" = None):
-    import torch
-    _require(args.device.type == "cuda", f"flex_attn_mixed_kv8 needs GPU tensors, not {args.device}")
-    with torch.cuda.device(args.device):
-        s = stream if stream is not None else current_stream()
-        check(lib().flex_attn_mixed_kv8(plan.handle, ctypes.byref(args), mode, s,
-                                        corun.handle if corun is not None else None), "flex_attn_mixed_kv8")
+    _run("flex_attn_mixed_kv8", args, stream, plan.handle, ctypes.byref(args), mode,
+         last=(corun.handle if corun is not None else None,))
 
 
 class Controller:
