@@ -217,10 +217,11 @@ __device__ __forceinline__ void turn_unit(const RopeParams& r, const Turn& t, fl
 }
 
 // Heads that one thread takes: it reads the cosines and sines of its unit once
-// for all of them, and their loads are in flight together. (One head a thread,
-// 2176 tokens of 28/4 heads of 128: 12.3 us against MEASURED_ROPE_MIXED; tokens on three axes
-// whose units have pairs of two of them: 25.4 against MEASURED_ROPE_AXES.)
-constexpr int kHeadsPerThread = 4;
+// for all of them, and their loads are in flight together. (1, 2 and 4 heads,
+// kernel times: 2176 tokens of 28/4 heads of 128 10.5, 9.9 and 9.9 us; 5900
+// tokens of 32/8 heads of 64 on three axes 21.2, 18.4 and 20.0; a 4096-token
+// latent prompt 257, 242 and 240; 64 tokens 3.6, 4.0 and 4.9.)
+constexpr int kHeadsPerThread = 2;
 
 // Unit j of heads h .. h + kHeadsPerThread - 1 of a token's n_heads rows, from
 // src(head) to dst(head) (a row's first column), written if live(); heads past
@@ -261,7 +262,7 @@ __device__ __forceinline__ void move_units(const RopeParams& r, const Positions<
 
 // ---------------------------------------------------------------------------
 // Into the bf16 cache: a work-group takes `per_wg` tokens; a thread takes one
-// unit of four consecutive heads (queries, then keys), or 32 bytes of values.
+// unit of two consecutive heads (queries, then keys), or 32 bytes of values.
 // Bound by HBM.
 // ---------------------------------------------------------------------------
 template <int DK, int DV, bool AXES>
@@ -312,7 +313,7 @@ __global__ __launch_bounds__(512) void rope_append_kernel(RopeAppendParams p) {
 // A wave holds its rows in registers between the maximum that gives the scale
 // and the conversion, so they are read once. (With all tasks of a block in the
 // work-group of its first token, a 2048-token chunk beside 128 decodes took
-// 33.6 us, now MEASURED_KV8_MIXED.)
+// 33.6 us, now 13.8.)
 // ---------------------------------------------------------------------------
 
 // The sequence that holds new token t: the largest s with query_start_loc[s]
