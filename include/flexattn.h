@@ -129,7 +129,8 @@ typedef struct flex_attn_plan_info {
   int32_t n_decode_seqs;     /* sequences with one new token (none in the 192/128 layout) */
   int32_t n_prefill_seqs;    /* sequences with two or more new tokens (one or more: 192/128) */
   int32_t n_decode_items;    /* decode pieces: (sequence, key range) work items */
-  int32_t n_prefill_items;   /* (sequence, row tile) work items */
+  int32_t n_prefill_items;   /* (sequence, row tile) work items; with kv_bits 8 a tile of a few
+                                on a long prefix may be cut along its keys into several */
   int32_t n_split_seqs;      /* decode sequences cut into more than one piece */
   int32_t decode_wg_width;   /* work-groups per decode range or piece (grid y) */
   int32_t n_decode_ranges;   /* balanced page ranges the decode pieces form */
@@ -140,7 +141,7 @@ typedef struct flex_attn_plan_info {
   int32_t bm;
   int32_t plan_words;        /* int32 words in the exported / uploaded plan */
   size_t device_plan_bytes;  /* bytes the device copy of the plan needs */
-  size_t workspace_bytes;    /* bytes of workspace decode needs (0 if none) */
+  size_t workspace_bytes;    /* bytes of workspace the run calls need (0 if none) */
   double decode_bytes;       /* algorithmic KV bytes of the decode phase */
   double prefill_flops;      /* algorithmic flops of the prefill phase */
   int32_t n_fused_wgs;       /* work-groups of the one-launch (FUSED) form; 0 when the
@@ -173,9 +174,9 @@ typedef struct flex_attn_plan_info {
  *  lse      fp32 [T, Hq] or NULL.
  *  d_plan   the plan uploaded with flex_attn_plan_upload.
  *  workspace  device scratch of >= flex_attn_plan_info.workspace_bytes (may
- *           be NULL when that is 0): the split decode items' partial results,
- *           written by the decode kernel and read by the merge kernel that
- *           follows it on the same stream. Its contents need no
+ *           be NULL when that is 0): the partial results of split decode items
+ *           and (8-bit caches) of cut prefill tiles, written by a phase's kernel
+ *           and read by the merge kernel that follows it on the same stream. Its contents need no
  *           initialisation. Two runs in flight at once must not share a
  *           workspace. */
 typedef struct flex_attn_args {
@@ -543,7 +544,8 @@ int flex_attn_kv8_append(const flex_attn_shape* shape, const flex_attn_rope* rop
 /* Attention over an 8-bit cache: flex_attn_decode, _prefill and _mixed with
  * cached values code * scale, on a plan made with kv_bits = 8. attn's caches
  * and strides are those of the 8-bit cache (strides in bytes, head strides
- * below 2^31 as well); everything else in it, outputs, workspace and debug mode included, is as for those calls.
+ * below 2^31 as well); everything else in it, outputs, workspace and debug mode
+ * included, is as for those calls.
  * FLEX_MODE_FUSED is FLEX_ERR_UNSUPPORTED. A NaN in a value row reaches the
  * queries that attend it and may reach others of the same tile of 32 keys of
  * that sequence; slots past a sequence's end never count. */

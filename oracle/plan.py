@@ -48,7 +48,15 @@ the contract is:
   F <= 3 * cus_prefill with cus_prefill < cus_total (a co-run share), else 32.
   Plans for 8-bit caches (kv_bits 8, grouped-query heads only) always take 128;
   their decode bytes count one byte a value and two scale bytes for each 16
-  tokens and KV head.
+  tokens and KV head. With N tiles of U_i = ceil(key_end / 64) units, for at
+  most half of the CUs (2 N * Hkv <= cus_prefill), and p >= 2 the least for
+  which Hkv * sum ceil(U_i / p) <= cus_prefill: if (max U_i - p) * 64 >= 384, a
+  tile is cut into n_i = ceil(U_i / p) pieces, the j-th over units
+  [floor(j U_i / n_i), floor((j + 1) U_i / n_i)); item words 5 to 7 hold its first key and, where
+  n_i > 1, n_i and its workspace slot (counted in tile order). Items are then
+  ordered by their keys' count, sequence, tile and first key, and a list of the
+  cut tiles (the item of each one's first piece, in item order) follows the
+  fused order.
 * co-run CU split: explicit, or (cus_decode = -1) the argmin over multiples of
   the granule of the step time, smallest n_d on ties: with t_p =
   prefill_flops / ((cus_total - n_d) * flops_cu) and r_s = min(hbm, n_d *
@@ -351,7 +359,10 @@ def build_plan(sh: Shape, opts: Optional[Opts], qsl: Sequence[int], seq_lens: Se
             r0, r1 = t * bm, min(rows, (t + 1) * bm)
             last_token = (r1 - 1) // G if flat else r1 - 1
             tiles.append([s, t, r0, r1, L - n + last_token + 1, 0, 0, 0])
-    tiles.sort(key=lambda it: (-it[4], it[0], it[1]))
+    n_pre_pieces = 0
+    if o.kv_bits == 8:
+        tiles, n_pre_pieces = cut_tiles(tiles, sh.num_kv_heads, cus_prefill)
+    tiles.sort(key=lambda it: (it[5] - it[4], it[0], it[1], it[5]))
 
     nd_, np_ = len(dec_items), len(tiles)
     order = sorted(range(nd_), key=lambda i: (-(dec_items[i][4] - dec_items[i][3]), i))
@@ -367,14 +378,15 @@ def build_plan(sh: Shape, opts: Optional[Opts], qsl: Sequence[int], seq_lens: Se
                         not mla and not split and G > 4 and W == 1 and heads_per_wg >= 3 and bm == 32,
                         G=G, sh=sh, o=o, cus_total=cus_total, cus_decode=cus_decode)
     off_fused = total
-    total += len(fused)
+    cut = [i for i, it in enumerate(tiles) if it[6] > 1 and it[5] == 0]
+    total += len(fused) + len(cut)
     off_lens = total
     total += 2 * B + 1
     hdr = [MAGIC, VERSION, B, nd_, np_, len(dec), len(pre), W, pre_height,
            HEADER, off_pre, ppr, cus_decode, cus_prefill, bm, total, R, off_ranges, off_order, off_merge,
            off_fused, len(fused), off_lens, RB]
     blob = (hdr + [x for it in dec_items for x in it] + ranges + order + merge + [x for it in tiles for x in it]
-            + fused + list(seq_lens) + list(qsl))
+            + fused + cut + list(seq_lens) + list(qsl))
     # workspace: (max, sum) per decode item, column and row, then the partial outputs;
     # only needed when some decode sequence is split
     if n_split == 0:
@@ -382,6 +394,8 @@ def build_plan(sh: Shape, opts: Optional[Opts], qsl: Sequence[int], seq_lens: Se
     else:
         stats = nd_ * W * rows_per_wg * 2 * 4
         ws = cdiv(stats, 256) * 256 + nd_ * W * rows_per_wg * sh.head_dim_v * 4
+    if n_pre_pieces:
+        ws = cdiv(ws, 256) * 256 + n_pre_pieces * sh.num_kv_heads * 128 * (2 + sh.head_dim_v) * 4
     info = dict(num_seqs=B, n_decode_seqs=len(dec), n_prefill_seqs=len(pre),
                 n_decode_items=nd_, n_prefill_items=np_, n_split_seqs=n_split, decode_wg_width=W,
                 n_decode_ranges=R, prefill_grid_y=pre_height, pages_per_split=ppr,
@@ -389,6 +403,30 @@ def build_plan(sh: Shape, opts: Optional[Opts], qsl: Sequence[int], seq_lens: Se
                 plan_words=total, device_plan_bytes=cdiv(total * 4, 256) * 256,
                 workspace_bytes=ws, decode_bytes=dec_bytes, prefill_flops=pre_flops, n_fused_wgs=len(fused))
     return PlanResult(OK, blob, info)
+
+
+def cut_tiles(tiles, kv_heads: int, cus: int):
+    """Prefill tiles of a plan for an 8-bit cache, those that would leave compute
+    units idle cut along their keys (see the module contract); and the pieces."""
+    units = [cdiv(t[4], 64) for t in tiles]
+    if not tiles or 2 * len(tiles) * kv_heads > cus:
+        return tiles, 0
+    piece = 2
+    while sum(cdiv(u, piece) for u in units) * kv_heads > cus:
+        piece += 1
+    if (max(units) - piece) * 64 < 384:
+        return tiles, 0
+    out, slot = [], 0
+    for t, u in zip(tiles, units):
+        n = cdiv(u, piece)
+        for j in range(n):
+            c = list(t)
+            c[5], c[4] = j * u // n * 64, min(t[4], (j + 1) * u // n * 64)
+            if n > 1:
+                c[6], c[7] = n, slot
+                slot += 1
+            out.append(c)
+    return out, slot
 
 
 def fused_order(tiles, grid_y: int, R: int, T: int, kv_heads_per_wg: int, fusable: bool, *, G: int,

@@ -135,6 +135,11 @@ int prepare(const flex_attn_plan_t* plan, const flex_attn_args* a, AttnParams* p
   if (kv8) {
     p->kv_scales = static_cast<const uint8_t*>(kv8->kv_scales);
     p->scale_sp = kv8->scale_page_stride;
+    if (plan->n_pre_pieces > 0) {
+      char* ws = static_cast<char*>(ws_override ? ws_override : a->workspace);
+      p->pre_stats = reinterpret_cast<float*>(ws + plan->pre_ws_offset);
+      p->pre_o = p->pre_stats + size_t(plan->n_pre_pieces) * sh.num_kv_heads * 128 * 2;
+    }
   }
   if (info.workspace_bytes > 0) {
     const int32_t W = info.decode_wg_width;
@@ -217,6 +222,10 @@ int run_prefill(const flex_attn_plan_t* plan, AttnParams p, const flex_attn_args
   p.items = static_cast<const int32_t*>(a->d_plan) + plan->words[H_OFF_PRE];
   p.n_items = info.n_prefill_items;
   p.grid_y = info.prefill_grid_y;
+  p.n_cus = info.cus_prefill;
+  p.longest_prefill = plan->longest_prefill;
+  p.n_cut_tiles = plan->n_cut_tiles;
+  p.cut_tiles = static_cast<const int32_t*>(a->d_plan) + plan->words[H_OFF_FUSED] + plan->words[H_N_FUSED];
   const hipError_t e = launch_prefill(p, plan->shape.head_dim_qk, info.bm, s);
   return e == hipSuccess ? FLEX_OK : hip_fail(e, "prefill launch");
 }

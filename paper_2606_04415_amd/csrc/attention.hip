@@ -730,33 +730,42 @@ struct RowParLoader<true, DQK, DV, NW, BN, NS, P> : LatentLoader<P, false> {
 };
 
 // Loader of tiles of 32 keys from an 8-bit cache, for work-groups of four
-// waves: codes pass through registers and become bf16 on their way into a stage
-// (converted once for the work-group; the waves' operand reads, of which each
-// wave makes as many as the tile holds, then see a bf16 tile). A load covers 64
-// 16-byte chunks, whole rows of K or of V, which all lie in one block of 16
-// keys: page, resource and scale are wave-uniform. fetch() starts the loads of
-// a tile, store() converts and writes what the last fetch() brought.
-template <int D, int P>
+// waves. Codes come by DMA into a ring of two raw tiles, and each wave converts
+// the part that it loaded into the bf16 tile of a stage (once for the
+// work-group; every wave's operand reads, of which each makes as many as the
+// tile holds, then see bf16). A load covers 64 16-byte chunks, whole rows of K
+// or of V, which all lie in one block of 16 keys: page, resource and scale are
+// wave-uniform. KG key groups of four waves have stages and raw tiles of their
+// own and one window of pages and scales between them.
+template <int D, int P, int KG>
 struct TileLoader8 {
   using C = RowParCfg<D, D, 4, 1, 32, false, 2>;
   static constexpr int CPR = D / 16;         // 16-byte chunks of codes in a row
+  static constexpr int RPL = 64 / CPR;       // rows of a load
   static constexpr int NL = 2 * 32 * CPR / 256;   // loads of a wave per tile: K then V (head dim 128), or K or V (64)
-  uint8_t* lds;
+  static constexpr int RAW = 2 * 32 * D;     // bytes of a raw tile
+  static constexpr int WIN = P == 16 ? 512 : 256;   // block-table entries of a window
+  static constexpr int BPP = P / 16;         // blocks of a page
+  // LDS: each group's two stages and two raw tiles, the window's pages, its
+  // blocks' scale bytes; at the end, the states of all groups but the first.
+  static constexpr int REGION = 2 * C::STAGE + 2 * RAW, PT_OFF = KG * REGION, SC_OFF = PT_OFF + 4 * WIN;
+  static constexpr int STATE = 4 * 64 * (2 * D + 16);   // of a group: 2 row blocks' accumulators, maxima and sums
+  static constexpr size_t LDS_BYTES = std::max<size_t>(SC_OFF + 2 * WIN * BPP, (KG - 1) * STATE);
+
+  uint8_t* lds;                              // the group's region
   const int* s_pt;
+  const uint16_t* s_sc;
   const uint8_t* base[NL];
-  const uint8_t* scales;
   uint32_t sp[NL], ss[NL], ld_off[NL], st_off[NL][2];
-  int64_t scale_sp;
-  int scale_row, key_end, row0;              // row0: first row of the wave's loads
+  int key_end, row0, lane, w;                // row0: first row of the wave's loads
   bool is_v[NL];
-  u32x4 x[NL];
+  u32x4 x[NL];                               // read_raw() to convert()
   uint32_t scale;
 
-  __device__ __forceinline__ TileLoader8(const AttnParams& p, int head, uint8_t* lds_, const int* s_pt_, int w, int lane,
-                                         int key_end_)
-      : lds(lds_), s_pt(s_pt_), scales(p.kv_scales + 2 * head), scale_sp(p.scale_sp), scale_row(2 * p.Hkv),
-        key_end(key_end_) {
-    constexpr int RPL = 64 / CPR;            // rows of a load
+  __device__ __forceinline__ TileLoader8(const AttnParams& p, int head, uint8_t* lds_, const int*, int w_, int lane_,
+                                         int key_end_, int group)
+      : lds(lds_ + group * REGION), s_pt(reinterpret_cast<const int*>(lds_ + PT_OFF)),
+        s_sc(reinterpret_cast<const uint16_t*>(lds_ + SC_OFF)), key_end(key_end_), lane(lane_), w(w_) {
     row0 = RPL * (w % (32 / RPL));
     const int row = row0 + lane / CPR, c = lane % CPR;
 #pragma unroll
@@ -766,29 +775,50 @@ struct TileLoader8 {
       base[j] = reinterpret_cast<const uint8_t*>(r.base) + int64_t(head) * r.sh;
       sp[j] = uint32_t(r.sp);
       ss[j] = uint32_t(r.ss);
-      ld_off[j] = uint32_t(lane / CPR) * ss[j] + 16u * uint32_t(c);
+      ld_off[j] = uint32_t(lane / CPR) * ss[j] + 16u * uint32_t(lane % CPR);
 #pragma unroll
       for (int h = 0; h < 2; ++h)
         st_off[j][h] = is_v[j] ? uint32_t(C::V_OFF + row * C::CPRV * 16 + 16 * swz_v<D>(2 * c + h, row))
                                : uint32_t(row * C::CPR * 16 + 16 * swz_k<D>(2 * c + h, row));
     }
   }
-  // Rows past key_end read zeros.
-  __device__ __forceinline__ void fetch(int kb, int pt_base) {
-    const int key = kb + row0;
-    const int rows = __builtin_amdgcn_readfirstlane(min(max(key_end - key, 0), 64 / CPR));
-    const int at = min(key, key_end - 1);
-    const uint32_t page = uint32_t(__builtin_amdgcn_readfirstlane(s_pt[at / P - pt_base]));
-#pragma unroll
-    for (int j = 0; j < NL; ++j) {
-      const auto r = __builtin_amdgcn_make_buffer_rsrc(
-          const_cast<uint8_t*>(base[j] + (uint64_t(page) * sp[j] + uint32_t(key % P) * ss[j])), 0,
-          __builtin_amdgcn_readfirstlane(int(uint32_t(rows) * ss[j])), kBufferFlags);
-      x[j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, int(ld_off[j]), 0, 0));
-    }
-    scale = *reinterpret_cast<const uint16_t*>(scales + (int64_t(page) * scale_sp + at % P / 16 * scale_row));
+  __device__ __forceinline__ uint8_t* raw(int slot, int j) const {
+    return lds + 2 * C::STAGE + slot * RAW + (w * NL + j) * 1024;
   }
-  __device__ __forceinline__ void store(int st) const {
+  // Start the loads of the tile at kb into a raw slot. Rows past key_end repeat
+  // the last key's (masked later). (A tile starts on a multiple of 32 keys, so
+  // at page 16 the wave's first slot in its page is the same in every tile.)
+  __device__ __forceinline__ int first_page(int kb, int pt_base) const {   // of the wave's loads
+    return s_pt[uint32_t(min(kb + row0, key_end - 1)) / P - uint32_t(pt_base)];
+  }
+  __device__ __forceinline__ void fetch(int kb, int slot, int first) const {
+    const uint32_t page = uint32_t(__builtin_amdgcn_readfirstlane(first));
+    const bool whole = kb + row0 + RPL <= key_end;
+    const int key = min(kb + row0, key_end - 1);
+    const uint32_t in_page = P == 16 && whole ? uint32_t(row0) % 16 : uint32_t(key) % P;
+    i32x4 r[NL];
+#pragma unroll
+    for (int j = 0; j < NL; ++j)
+      r[j] = uniform_rsrc(base[j] + (uint64_t(page) * sp[j] + in_page * ss[j]), uint32_t(RPL) * ss[j]);
+    if (whole) {
+#pragma unroll
+      for (int j = 0; j < NL; ++j) dma16_buf(r[j], ld_off[j], raw(slot, j));
+    } else {
+      const uint32_t row = uint32_t(min(lane / CPR, key_end - 1 - key));
+#pragma unroll
+      for (int j = 0; j < NL; ++j) dma16_buf(r[j], row * ss[j] + 16u * uint32_t(lane % CPR), raw(slot, j));
+    }
+  }
+  // The wave's part of the raw tile at kb, whose loads have landed, into
+  // registers; then as bf16 into a stage.
+  __device__ __forceinline__ void read_raw(int kb, int slot, int pt_base) {
+    uint32_t block = uint32_t(min(kb + row0, key_end - 1)) / 16 - uint32_t(pt_base * BPP);
+    asm volatile("" : "+v"(block));   // read into a vector register: a scalar one would be waited for here
+    scale = s_sc[block];
+#pragma unroll
+    for (int j = 0; j < NL; ++j) x[j] = *reinterpret_cast<const u32x4*>(raw(slot, j) + 16 * lane);
+  }
+  __device__ __forceinline__ void convert(int st) const {
     uint8_t* stage = lds + st * C::STAGE;
 #pragma unroll
     for (int j = 0; j < NL; ++j) {
@@ -798,20 +828,13 @@ struct TileLoader8 {
     }
   }
 };
-template <bool VALIAS, int DQK, int DV, int NW, int BN, int NS, int P, bool KV8>
-struct LoaderOf {
-  using type = RowParLoader<VALIAS, DQK, DV, NW, BN, NS, P>;
-};
-template <int D, int P>
-struct LoaderOf<false, D, D, 4, 32, 2, P, true> {
-  using type = TileLoader8<D, P>;
-};
 
 // One work-group's work: item `item` of the phase, column `col`, threads
-// 0 .. NW*64-1 of the work-group, the work-group's dynamic LDS. KV8: an 8-bit
-// cache.
-template <int DQK, int DV, int NW, int RB, int BN, bool VALIAS, int MODE, int P, int NS, int TB, bool KV8 = false>
+// 0 .. NW*64-1 of the work-group, the work-group's dynamic LDS. KG > 0: an 8-bit
+// cache, and KG times NW waves, in groups that take every KG-th key tile.
+template <int DQK, int DV, int NW, int RB, int BN, bool VALIAS, int MODE, int P, int NS, int TB, int KG = 0>
 __device__ __forceinline__ void rowpar_body(const AttnParams& p, int item, int col) {
+  constexpr bool KV8 = KG > 0;
   using C = RowParCfg<DQK, DV, NW, RB, BN, VALIAS, NS>;
   static_assert(NS >= 2 && NS <= 6, "stages");
   static_assert(BN % 32 == 0, "whole 32-key chunks per tile");
@@ -821,7 +844,8 @@ __device__ __forceinline__ void rowpar_body(const AttnParams& p, int item, int c
 
   const int tid = threadIdx.x;
   const int lane = tid & 63;
-  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int w = KG > 1 ? wave % NW : wave, group = KG > 1 ? wave / NW : 0;
   const int n = lane & 15, gq = lane >> 4;
   const int32_t* it = p.items + 8 * (MODE == kDecodeLatent ? p.order[item] : item);
   const int seq = it[0];
@@ -870,7 +894,7 @@ __device__ __forceinline__ void rowpar_body(const AttnParams& p, int item, int c
     wave_full = L - nq + wr0 + 1;
   } else if constexpr (MODE == kPrefillFlat) {
     const int r0 = it[2], r1 = it[3];
-    key_begin = 0;
+    key_begin = KV8 ? it[5] : 0;
     key_end = it[4];
     head_kv = col;
     const int G = p.G;
@@ -948,7 +972,11 @@ __device__ __forceinline__ void rowpar_body(const AttnParams& p, int item, int c
   }
   const u32x4 ones = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};   // bf16 1.0 x 8
 
-  typename LoaderOf<VALIAS, DQK, DV, NW, BN, NS, P, KV8>::type loader(p, head_kv, lds, s_pt, w, lane, key_end);
+  auto make_loader = [&] {
+    if constexpr (KV8) return TileLoader8<DQK, P, KG>(p, head_kv, lds, s_pt, w, lane, key_end, group);
+    else return RowParLoader<VALIAS, DQK, DV, NW, BN, NS, P>(p, head_kv, lds, s_pt, w, lane, key_end);
+  };
+  auto loader = make_loader();
   auto issue = [&](int kb, int st, int pt_base) {
     if constexpr (!KV8) loader.issue(kb, st, pt_base);
   };
@@ -995,13 +1023,18 @@ __device__ __forceinline__ void rowpar_body(const AttnParams& p, int item, int c
         reinterpret_cast<const uint16_t*>(base + ((32 * ch + 16 * half) * VROW + (VALIAS ? 32 * cv : 0))));
   };
 
+  auto none = [] {};
+  int region = 0;   // LDS offset of the wave's stages
+  if constexpr (KV8) region = group * TileLoader8<DQK, P, KG>::REGION;
+
   // One key tile: S^T = K Q^T per 32-key chunk, masking (only when the tile
   // crosses a row limit), the tile max of each row, lazy rescale, then
   // probabilities and O += P V, l += P 1 per chunk. (One instance per loop:
   // a masked and an unmasked copy in one loop body would be merged by the
   // compiler at a large register cost.)
-  auto compute_tile = [&](bool masked, int st, int kc0) {
-    const uint8_t* stage = lds + __builtin_amdgcn_readfirstlane(st * C::STAGE);
+  // (scored() runs behind the scores' products, for work that hides there.)
+  auto compute_tile = [&](bool masked, int st, int kc0, auto&& scored) {
+    const uint8_t* stage = lds + __builtin_amdgcn_readfirstlane(st * C::STAGE + region);
     f32x4 s[RB][2 * CH];
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb)
@@ -1046,6 +1079,8 @@ __device__ __forceinline__ void rowpar_body(const AttnParams& p, int item, int c
       // read of the tile to the top would cost a register per value.
       __builtin_amdgcn_sched_barrier(0);
     }
+
+    scored();
 
     // s[rb][2ch + b][r] is the score of key kc0 + 32ch + 16b + 4gq + r for row n.
     float cmax[RB];
@@ -1158,10 +1193,107 @@ __device__ __forceinline__ void rowpar_body(const AttnParams& p, int item, int c
   // with tile kt - 1, so its stage takes tile kt + NS - 1) and computes.
   // Tiles that no row of the wave masks and that still have a tile to issue
   // after them run in a loop with fixed wait counts and no masking.
+  if constexpr (KV8) {
+    // Past the barrier of step kt (every wave has written its part of the
+    // group's tile and is done with the one before) the group's next tile is
+    // converted to where the last one was, between the parts of this one, and
+    // the loads of the third one on start into its raw slot; those of the
+    // second are in flight. The same windows of block-table entries as below,
+    // with the scales of their blocks.
+    using L8 = TileLoader8<DQK, P, KG>;
+    int* const pt = reinterpret_cast<int*>(lds + L8::PT_OFF);
+    uint16_t* const sc = reinterpret_cast<uint16_t*>(lds + L8::SC_OFF);
+    const int last = key_end > 0 ? (key_end - 1) / P : 0;
+    for (int wk0 = key_begin; wk0 < key_end; wk0 += L8::WIN * P) {
+      const int wk1 = min(key_end, wk0 + L8::WIN * P), pt_base = wk0 / P, tiles = (wk1 - wk0 + BN - 1) / BN;
+      const int pages = min(L8::WIN, last + 1 - pt_base);
+      const int ntiles = (tiles - group + KG - 1) / KG, steps = (tiles + KG - 1) / KG;   // the group's; the longest group's
+      auto key_of = [&](int kt) { return wk0 + (kt * KG + group) * BN; };
+      lds_barrier();
+      for (int i = tid; i < pages; i += KG * C::NT) pt[i] = bt_row[pt_base + i];
+      wait_vmem_all();
+      lds_barrier();
+      if (ntiles > 0) loader.fetch(key_of(0), 0, loader.first_page(key_of(0), pt_base));
+      if (ntiles > 1) loader.fetch(key_of(1), 1, loader.first_page(key_of(1), pt_base));
+      for (int i = tid; i < pages * L8::BPP; i += KG * C::NT)
+        sc[i] = *reinterpret_cast<const uint16_t*>(p.kv_scales + int64_t(pt[i / L8::BPP]) * p.scale_sp +
+                                                   (i % L8::BPP * p.Hkv + head_kv) * 2);
+      wait_vmem_all();
+      lds_barrier();
+      if (ntiles > 0) {
+        loader.read_raw(key_of(0), 0, pt_base);
+        loader.convert(0);
+      }
+      if (ntiles > 2) loader.fetch(key_of(2), 0, loader.first_page(key_of(2), pt_base));
+      // Tiles that no row of the wave masks.
+      const int steady = wave_on ? min(max(0, wave_full - wk0) / BN - group + KG - 1, tiles) / KG : 0;
+      int kt = 0;
+      for (; kt < min(steady, ntiles - 3); ++kt) {
+        lds_barrier();
+        wait_vmem<L8::NL>();
+        __atomic_signal_fence(__ATOMIC_SEQ_CST);   // the reads of the raw tile stay behind the wait
+        const int page = loader.first_page(key_of(kt + 3), pt_base);
+        loader.read_raw(key_of(kt + 1), (kt + 1) & 1, pt_base);
+        compute_tile(false, kt & 1, key_of(kt), [&] {
+          loader.convert((kt + 1) & 1);
+          loader.fetch(key_of(kt + 3), (kt + 1) & 1, page);
+        });
+      }
+      for (; kt < steps; ++kt) {
+        const int kc = key_of(kt);
+        lds_barrier();
+        if (kt + 1 < ntiles) {
+          if (kt + 2 < ntiles) wait_vmem<L8::NL>();
+          else wait_vmem<0>();
+          __atomic_signal_fence(__ATOMIC_SEQ_CST);
+          loader.read_raw(key_of(kt + 1), (kt + 1) & 1, pt_base);
+          loader.convert((kt + 1) & 1);
+          if (kt + 3 < ntiles) loader.fetch(key_of(kt + 3), (kt + 1) & 1, loader.first_page(key_of(kt + 3), pt_base));
+        }
+        if (kt < ntiles && wave_on && kc < wave_limit) compute_tile(kc + BN > wave_full, kt & 1, kc, none);
+      }
+    }
+    // The groups' states meet in the first: row maxima and sums, accumulators
+    // scaled to the common maximum, in group order.
+    if constexpr (KG > 1) {
+      static_assert(RB == 2, "the state holds two row blocks");
+      lds_barrier();
+      auto state = [&](int g) { return lds + (g - 1) * L8::STATE + w * (L8::STATE / 4) + 16 * lane; };
+      if (group > 0) {
+        uint8_t* at = state(group);
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+          for (int a = 0; a < C::NACC; ++a) *reinterpret_cast<f32x4*>(at + (rb * C::NACC + a) * 1024) = o[rb][a];
+        *reinterpret_cast<f32x4*>(at + RB * C::NACC * 1024) = f32x4{m[0], m[RB - 1], lpart[0], lpart[RB - 1]};
+      }
+      lds_barrier();
+      if (group > 0) return;
+#pragma unroll 1
+      for (int g = 1; g < KG; ++g) {
+        const uint8_t* at = state(g);
+        const f32x4 ml = *reinterpret_cast<const f32x4*>(at + RB * C::NACC * 1024);
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+          const float mg = ml[rb], M = fmaxf(m[rb], mg);
+          const float f0 = fast_exp2(m[rb] - M), f1 = fast_exp2(mg - M);
+          m[rb] = M;
+          lpart[rb] = lpart[rb] * f0 + ml[2 + rb] * f1;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const float a0 = shfl_f(f0, 4 * gq + r), a1 = shfl_f(f1, 4 * gq + r);
+#pragma unroll
+            for (int a = 0; a < C::NACC; ++a)
+              o[rb][a][r] = o[rb][a][r] * a0 + reinterpret_cast<const float*>(at + (rb * C::NACC + a) * 1024)[r] * a1;
+          }
+        }
+      }
+    }
+  }
   constexpr int WIN_KEYS = kPageWin * P;
   static_assert(WIN_KEYS % BN == 0, "windows hold whole tiles");
   const int last_page = key_end > 0 ? (key_end - 1) / P : 0;
-  for (int wk0 = key_begin; wk0 < key_end; wk0 += WIN_KEYS) {
+  for (int wk0 = key_begin; !KV8 && wk0 < key_end; wk0 += WIN_KEYS) {
     const int wk1 = min(key_end, wk0 + WIN_KEYS);
     const int pt_base = wk0 / P;
     lds_barrier();
@@ -1172,34 +1304,6 @@ __device__ __forceinline__ void rowpar_body(const AttnParams& p, int item, int c
     wait_vmem_all();
     lds_barrier();
     const int ntiles = (wk1 - wk0 + BN - 1) / BN;
-    if constexpr (KV8) {
-      // Two stages, the codes of one more tile in registers: past the barrier
-      // of tile kt (every wave has written its part of it and is done with
-      // tile kt - 1) tile kt + 1 is written where tile kt - 1 was, the loads of
-      // tile kt + 2 start, and run under the products of tile kt.
-      loader.fetch(wk0, pt_base);
-      loader.store(0);
-      if (ntiles > 1) loader.fetch(wk0 + BN, pt_base);
-      auto next = [&](int kt) {
-        lds_barrier();
-        if (kt + 1 < ntiles) loader.store((kt + 1) & 1);
-        if (kt + 2 < ntiles) loader.fetch(wk0 + (kt + 2) * BN, pt_base);
-        __builtin_amdgcn_sched_barrier(0);
-      };
-      const int steady = wave_on ? min(max(0, wave_full - wk0) / BN, ntiles) : 0;
-      int kt = 0;
-      for (; kt < steady; ++kt) {
-        next(kt);
-        compute_tile(false, kt & 1, wk0 + kt * BN);
-      }
-      for (; kt < ntiles; ++kt) {
-        const int kc = wk0 + kt * BN;
-        next(kt);
-        if (!wave_on || kc >= wave_limit) continue;
-        compute_tile(true, kt & 1, kc);
-      }
-      continue;
-    }
 #pragma unroll
     for (int t = 0; t < NS - 1; ++t)
       if (t < ntiles) issue(wk0 + t * BN, t, pt_base);
@@ -1212,7 +1316,7 @@ __device__ __forceinline__ void rowpar_body(const AttnParams& p, int item, int c
       wait_vmem<(NS - 2) * C::NI>();
       lds_barrier();
       issue(wk0 + (kt + NS - 1) * BN, (kt + NS - 1) % NS, pt_base);
-      compute_tile(false, kt % NS, wk0 + kt * BN);
+      compute_tile(false, kt % NS, wk0 + kt * BN, none);
     }
     for (; kt < ntiles; ++kt) {
       const int kc = wk0 + kt * BN;
@@ -1220,7 +1324,7 @@ __device__ __forceinline__ void rowpar_body(const AttnParams& p, int item, int c
       lds_barrier();
       if (kt + NS - 1 < ntiles) issue(wk0 + (kt + NS - 1) * BN, (kt + NS - 1) % NS, pt_base);
       if (!wave_on || kc >= wave_limit) continue;   // past this wave's rows: loads and barriers only
-      compute_tile(kc + BN > wave_full, kt % NS, kc);
+      compute_tile(kc + BN > wave_full, kt % NS, kc, none);
     }
   }
 
@@ -1233,6 +1337,28 @@ __device__ __forceinline__ void rowpar_body(const AttnParams& p, int item, int c
   if constexpr (MODE != kDecodeLatent) {
     if (!wave_on) return;
     const int r0 = it[2], r1 = it[3];
+    if constexpr (KV8) {
+      if (it[6] > 1) {   // a piece of the tile's keys: its state, for the merge
+        const int64_t row0 = (int64_t(it[7]) * p.Hkv + head_kv) * 128;
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int i = (w * RB + rb) * 16 + 4 * gq + r;
+            const float mr = shfl_f(m[rb], 4 * gq + r), lr = shfl_f(ltot[rb], 4 * gq + r);
+            if (r0 + i >= r1) continue;
+            float* dst = p.pre_o + (row0 + i) * DV + n;
+#pragma unroll
+            for (int cv = 0; cv < C::NACC; ++cv) dst[16 * cv] = o[rb][cv][r];
+            if (n == 0) {
+              p.pre_stats[(row0 + i) * 2] = mr;
+              p.pre_stats[(row0 + i) * 2 + 1] = lr;
+            }
+          }
+        }
+        return;
+      }
+    }
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
       const int blk = MODE == kPrefillGrouped ? ((w % TB) * RB + rb) : (w * RB + rb);
@@ -1325,8 +1451,8 @@ void rowpar_kernel(AttnParams p) {
 // per SIMD are the register budget the compiler is held to, so that
 // 4 * WPE / NW work-groups share a compute unit and their barriers drift
 // apart. 1-D XCD-aware grid as for kPrefillGrouped.
-template <int D, int NW, int RB, int BN, int P, int NS, int WPE, bool KV8 = false>
-__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(WPE)))
+template <int D, int NW, int RB, int BN, int P, int NS, int WPE, int KG = 0>
+__global__ __launch_bounds__(NW * 64 * (KG > 1 ? KG : 1)) __attribute__((amdgpu_waves_per_eu(WPE)))
 void flat_prefill_kernel(AttnParams p) {
   int item = int(blockIdx.x), col = int(blockIdx.y);
   if (p.xcd_remap) {
@@ -1335,7 +1461,7 @@ void flat_prefill_kernel(AttnParams p) {
     item = j * (8 / p.grid_y) + x / p.grid_y;
     if (item >= p.n_items) return;
   }
-  rowpar_body<D, D, NW, RB, BN, false, kPrefillFlat, P, NS, 1, KV8>(p, item, col);
+  rowpar_body<D, D, NW, RB, BN, false, kPrefillFlat, P, NS, 1, KG>(p, item, col);
 }
 
 // Per-head prefill with split-out heads (keys 192, values 128): tiles of 128
@@ -1619,13 +1745,15 @@ static hipError_t launch_perhead_t(const AttnParams& p, dim3 grid, hipStream_t s
   return hipGetLastError();
 }
 
-template <int D, int NW, int RB, int BN, int P, int NS, int WPE, bool KV8 = false>
+template <int D, int NW, int RB, int BN, int P, int NS, int WPE, int KG = 0>
 static hipError_t launch_flat_t(const AttnParams& p, dim3 grid, hipStream_t stream) {
   using C = RowParCfg<D, D, NW, RB, BN, false, NS>;
-  auto kern = flat_prefill_kernel<D, NW, RB, BN, P, NS, WPE, KV8>;
-  const hipError_t attr = set_dynamic_lds(reinterpret_cast<const void*>(kern), C::LDS_BYTES);
+  size_t lds = C::LDS_BYTES;
+  if constexpr (KG > 0) lds = TileLoader8<D, P, KG>::LDS_BYTES;
+  auto kern = flat_prefill_kernel<D, NW, RB, BN, P, NS, WPE, KG>;
+  const hipError_t attr = set_dynamic_lds(reinterpret_cast<const void*>(kern), lds);
   if (attr != hipSuccess) return attr;
-  hipLaunchKernelGGL(kern, grid, dim3(C::NT), C::LDS_BYTES, stream, p);
+  hipLaunchKernelGGL(kern, grid, dim3(C::NT * (KG > 1 ? KG : 1)), lds, stream, p);
   return hipGetLastError();
 }
 
@@ -1636,9 +1764,17 @@ static hipError_t launch_flat_t(const AttnParams& p, dim3 grid, hipStream_t stre
 // compute unit and their barriers drift apart.
 template <int D, int P>
 static hipError_t launch_prefill_flat(const AttnParams& p, int bm, dim3 grid, hipStream_t stream) {
-  if (bm == 128)
-    return p.kv_scales ? launch_flat_t<D, 4, 2, 32, P, 2, 3, true>(p, grid, stream)
-                       : launch_flat_t<D, 4, 2, 32, P, 3, 3>(p, grid, stream);
+  if (bm == 128 && p.kv_scales) {
+    // Two key groups where work-groups have a compute unit each to themselves
+    // and tiles to share (28/4 heads of 128, one group against two: a prompt of
+    // 512 22.9 and 19.4 us, of 1024 on 4000 keys 155 and 107, but of 64 8.4 and
+    // 9.3, and 8 of 256, 448 work-groups, 17.8 and 23.0).
+    const bool pairs = int64_t(p.n_items) * p.grid_y <= p.n_cus && p.longest_prefill >= 256;
+    const hipError_t e = pairs ? launch_flat_t<D, 4, 2, 32, P, 2, 2, 2>(p, grid, stream)
+                               : launch_flat_t<D, 4, 2, 32, P, 2, 3, 1>(p, grid, stream);
+    return e != hipSuccess || p.n_cut_tiles == 0 ? e : launch_merge_tiles(p, D, stream);
+  }
+  if (bm == 128) return launch_flat_t<D, 4, 2, 32, P, 3, 3>(p, grid, stream);
   return hipErrorInvalidValue;
 }
 

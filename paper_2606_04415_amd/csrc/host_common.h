@@ -11,8 +11,9 @@ namespace flexattn {
 
 // Plan word layout: a 24-word header, 8 words per decode item, the range
 // table (the decode tail's ranges last; H_N_TAIL_RANGES of them), the piece launch order, the merge list, 8 words per prefill item,
-// the fused order, then the batch's seq_lens [B] and query_start_loc [B+1]
-// as the plan saw them (the debug check compares the device copies with
+// the fused order, the list of cut prefill tiles (8-bit caches: the item of
+// each one's first piece), then the batch's seq_lens [B] and query_start_loc
+// [B+1] as the plan saw them (the debug check compares the device copies with
 // them).
 constexpr int32_t kPlanMagic = 0x46504C58;
 constexpr int32_t kPlanVersion = 7;
@@ -36,7 +37,9 @@ enum HeaderField {
 // work-group per piece; the merge list after that holds, for each decode
 // sequence cut into several pieces (batch order), the index of its first
 // piece.
-// Prefill item words: seq, tile, row_begin, row_end, key_end, unused x3.
+// Prefill item words: seq, tile, row_begin, row_end, key_end, and for 8-bit
+// caches key_begin, pieces of the tile (0: whole), this piece's workspace slot
+// (a tile's slots are consecutive); else 0 x3.
 // Fused order (one launch for both phases, FLEX_MODE_FUSED): entry b is the
 // work of launch work-group b: e < n_pre_items * prefill_grid_y is prefill
 // work-group e (tile e / grid_y, column e % grid_y); e >= that is decode
@@ -93,6 +96,14 @@ constexpr double kTailMinPrefillUs = 100.0;
 
 // Tokens that share one scale of an 8-bit cache (pages hold whole blocks).
 constexpr int kKv8Block = 16;
+// Pieces of prefill tiles over an 8-bit cache (plan.cpp): their unit, the
+// shortest one and the least gain, in keys. 28/4 heads of 128, whole tiles and
+// cut ones, merge included, us: 2 tokens on 500 keys 16.6 and 10.9, 64 on 600
+// 22.8 and 15.2, on 4000 88 and 26, 2 prompts of 200 on 800 29.7 and 28.1, on
+// 2400 61 and 44; with a shortest piece of 256 the first two take 13.5 and
+// 16.4. Where 320 keys and 256 are gained: 4 prompts of 128 on 500 22.0 and
+// 25.8, one of 512 19.6 and 20.9.
+constexpr int64_t kKv8PieceKeys = 64, kKv8MinPiece = 128, kKv8PieceGain = 384;
 
 // Rows (query heads) one decode work-group owns in the 576/512 layout.
 constexpr int kLatentRowsPerWG = 64;       // latent heads must be a multiple of this
@@ -113,6 +124,10 @@ struct flex_attn_plan {
   int32_t rows_per_wg;      // query rows of one decode work-group
   int32_t kv_bits;          // 16: bf16 caches, 8: e4m3 caches with block scales
   int32_t max_pages_per_seq;  // block-table entries a row must hold
+  size_t pre_ws_offset;     // 8-bit caches: bytes of the workspace before the prefill pieces' part
+  int32_t n_pre_pieces;     // pieces of cut prefill tiles
+  int32_t n_cut_tiles;      // cut prefill tiles
+  int32_t longest_prefill;  // most keys of a prefill item
   std::vector<int32_t> words;
 };
 

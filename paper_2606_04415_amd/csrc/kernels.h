@@ -39,6 +39,12 @@ struct AttnParams {
   float scale_log2;       // sm_scale * log2(e)
   const uint8_t* kv_scales;   // 8-bit caches: scale bytes, [page][block of 16 slots][kv head][K, V]
   int64_t scale_sp;           // bytes from page to page
+  float* pre_stats;           // 8-bit caches, prefill pieces: [slot][kv head][128][2] (max in log2 units, sum)
+  float* pre_o;               // [slot][kv head][128][d_v] unnormalised partial outputs
+  const int32_t* cut_tiles;   // item of the first piece of every cut tile
+  int32_t n_cut_tiles;        // 0: no tile is cut
+  int32_t n_cus;              // prefill: compute units of its share
+  int32_t longest_prefill;    // most keys of an item
 };
 
 // Allow a kernel the dynamic LDS it launches with. The attribute is set on
@@ -53,6 +59,8 @@ hipError_t launch_decode(const AttnParams& p, int head_dim_qk, bool has_splits, 
 hipError_t launch_decode_merge(const AttnParams& p, int head_dim_qk, hipStream_t stream);
 // Grouped-query decode over an 8-bit cache, without the merge (decode_kv8.hip).
 hipError_t launch_decode_kv8(const AttnParams& p, int head_dim, hipStream_t stream);
+// Joins the pieces of cut prefill tiles.
+hipError_t launch_merge_tiles(const AttnParams& p, int head_dim, hipStream_t stream);
 hipError_t launch_merge_many(const AttnParams& p, int head_dim, hipStream_t stream);
 // Latent rows in groups of 128 (latent.hip).
 hipError_t launch_latent128(const AttnParams& p, bool decode, dim3 grid, hipStream_t stream);

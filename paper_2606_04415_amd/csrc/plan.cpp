@@ -369,7 +369,7 @@ extern "C" int flex_attn_plan(const flex_attn_shape* shape, const flex_attn_plan
   // a token, or with flat tiles a (token, query head) pair of one KV head,
   // r = token * G + head; a tile's key range ends at the causal limit of its
   // last row's token.
-  struct Tile { int32_t s, t, r0, r1, kend; };
+  struct Tile { int32_t s, t, r0, r1, kend, kbeg, pieces, slot; };
   std::vector<Tile> tiles;
   for (int32_t s : pre) {
     const int32_t n = qsl[s + 1] - qsl[s], L = seq_lens[s];
@@ -377,13 +377,48 @@ extern "C" int flex_attn_plan(const flex_attn_shape* shape, const flex_attn_plan
     if (rows > INT32_MAX) return set_error(FLEX_ERR_INVALID_ARG, "prefill chunk too long for flat row tiles");
     for (int32_t t = 0; int64_t(t) * bm < rows; ++t) {
       const int32_t r0 = t * bm, r1 = int32_t(std::min<int64_t>(rows, int64_t(t + 1) * bm));
-      tiles.push_back({s, t, r0, r1, L - n + (flat ? (r1 - 1) / G + 1 : r1)});
+      tiles.push_back({s, t, r0, r1, L - n + (flat ? (r1 - 1) / G + 1 : r1), 0, 0, 0});
+    }
+  }
+  // Over an 8-bit cache, tiles that would leave half of the compute units idle
+  // are cut along their keys too (pieces of whole kKv8PieceKeys, joined by a
+  // merge that follows the prefill): into the shortest pieces of at least
+  // kKv8MinPiece keys that have a compute unit each, when that shortens the
+  // longest tile by kKv8PieceGain keys or more. (The first piece of a tile has
+  // key_begin 0.)
+  int32_t n_pre_pieces = 0;   // of cut tiles
+  if (kv8 && !tiles.empty() && 2 * int64_t(tiles.size()) * sh.num_kv_heads <= cus_prefill) {
+    int64_t longest = 0, piece = kKv8MinPiece / kKv8PieceKeys;   // in units of kKv8PieceKeys
+    for (const Tile& t : tiles) longest = std::max(longest, cdiv(t.kend, kKv8PieceKeys));
+    auto work_groups = [&] {
+      int64_t n = 0;
+      for (const Tile& t : tiles) n += cdiv(cdiv(t.kend, kKv8PieceKeys), piece);
+      return n * sh.num_kv_heads;
+    };
+    while (work_groups() > cus_prefill) ++piece;
+    if ((longest - piece) * kKv8PieceKeys >= kKv8PieceGain) {
+      std::vector<Tile> cut;
+      for (const Tile& t : tiles) {
+        const int64_t units = cdiv(t.kend, kKv8PieceKeys), pieces = cdiv(units, piece);
+        for (int64_t j = 0; j < pieces; ++j) {
+          Tile c = t;
+          c.kbeg = int32_t(j * units / pieces * kKv8PieceKeys);
+          c.kend = int32_t(std::min<int64_t>(t.kend, (j + 1) * units / pieces * kKv8PieceKeys));
+          if (pieces > 1) {
+            c.pieces = int32_t(pieces);
+            c.slot = n_pre_pieces++;
+          }
+          cut.push_back(c);
+        }
+      }
+      tiles.swap(cut);
     }
   }
   std::stable_sort(tiles.begin(), tiles.end(), [](const Tile& a, const Tile& b) {
-    if (a.kend != b.kend) return a.kend > b.kend;
+    if (a.kend - a.kbeg != b.kend - b.kbeg) return a.kend - a.kbeg > b.kend - b.kbeg;
     if (a.s != b.s) return a.s < b.s;
-    return a.t < b.t;
+    if (a.t != b.t) return a.t < b.t;
+    return a.kbeg < b.kbeg;
   });
 
   // Fused order for FLEX_MODE_FUSED (its layout and rule are described with
@@ -479,7 +514,13 @@ extern "C" int flex_attn_plan(const flex_attn_shape* shape, const flex_attn_plan
   const int32_t off_merge = off_order + n_dec_items;
   const int32_t off_pre = off_merge + int32_t(merge_list.size());
   const int32_t off_fused = off_pre + kItemWords * n_pre_items;
-  const int32_t off_lens = off_fused + int32_t(fused.size());
+  // The first piece of every cut prefill tile (8-bit caches, which have no
+  // fused order) stands behind the fused order.
+  std::vector<int32_t> cut_list;
+  for (int32_t i = 0; i < n_pre_items; ++i)
+    if (tiles[i].pieces > 1 && tiles[i].kbeg == 0) cut_list.push_back(i);
+  plan->n_cut_tiles = int32_t(cut_list.size());
+  const int32_t off_lens = off_fused + int32_t(fused.size() + cut_list.size());
   const int32_t total = off_lens + 2 * num_seqs + 1;
   auto& w = plan->words;
   w.assign(kHeaderWords, 0);
@@ -512,10 +553,11 @@ extern "C" int flex_attn_plan(const flex_attn_shape* shape, const flex_attn_plan
   w.insert(w.end(), order.begin(), order.end());
   w.insert(w.end(), merge_list.begin(), merge_list.end());
   for (const Tile& t : tiles) {
-    const int32_t item[kItemWords] = {t.s, t.t, t.r0, t.r1, t.kend, 0, 0, 0};
+    const int32_t item[kItemWords] = {t.s, t.t, t.r0, t.r1, t.kend, t.kbeg, t.pieces, t.slot};
     w.insert(w.end(), item, item + kItemWords);
   }
   w.insert(w.end(), fused.begin(), fused.end());
+  w.insert(w.end(), cut_list.begin(), cut_list.end());
   w.insert(w.end(), seq_lens, seq_lens + num_seqs);
   w.insert(w.end(), qsl, qsl + num_seqs + 1);
 
@@ -526,6 +568,12 @@ extern "C" int flex_attn_plan(const flex_attn_shape* shape, const flex_attn_plan
     const size_t stats = size_t(n_dec_items) * W * rows_per_wg * 2 * 4;
     ws = size_t(cdiv(int64_t(stats), 256) * 256) + size_t(n_dec_items) * W * rows_per_wg * sh.head_dim_v * 4;
   }
+  // Behind it, per (piece of a cut prefill tile, KV head) the same of its 128 rows.
+  plan->pre_ws_offset = size_t(cdiv(int64_t(ws), 256) * 256);
+  plan->n_pre_pieces = n_pre_pieces;
+  plan->longest_prefill = 0;
+  for (const Tile& t : tiles) plan->longest_prefill = std::max(plan->longest_prefill, t.kend - t.kbeg);
+  if (n_pre_pieces > 0) ws = plan->pre_ws_offset + size_t(n_pre_pieces) * sh.num_kv_heads * 128 * (2 + sh.head_dim_v) * 4;
   flex_attn_plan_info& info = plan->info;
   std::memset(&info, 0, sizeof(info));
   info.num_seqs = num_seqs;

@@ -190,6 +190,57 @@ def test_long_context_and_far_pages():
     assert torch.equal(again[0].view(torch.int16), out[0].view(torch.int16)) and torch.equal(again[1], out[1])
 
 
+@pytest.mark.parametrize("hq,hkv,d,P,ns,ls", [
+    (28, 4, 128, 16, [64], [4064]), (28, 4, 128, 64, [2, 20], [700, 1003]), (4, 1, 64, 16, [130, 1, 3], [1500, 40, 8300]),
+    (32, 8, 64, 64, [33, 5], [900, 5]), (6, 3, 64, 64, [2], [385]), (16, 1, 128, 16, [300], [300]), (16, 1, 128, 16, [450], [450])])
+def test_prefill_tiles_cut_along_their_keys(hq, hkv, d, P, ns, ls):
+    """Few tiles: pieces of keys, whose rows may see none of a piece's, joined by a merge; other tiles stay whole
+    (so do tiles of 448 keys or less, in two cases)."""
+    log(f"kv8 cut prefill {hq}/{hkv} d{d} page {P} {ns} {ls}")
+    c = Case(hq, hkv, d, P, ns, ls, seed=hq + P, spread=6)
+    pa = c.plan()
+    tiles = sum(-(-n * (hq // hkv) // 128) for n in ns if n > 1)
+    assert (pa.plan.info["n_prefill_items"] > tiles) == (max(ls) > 448)
+    out = c.run("prefill", pa=pa)
+    single = torch.from_numpy(np.repeat(np.array(ns) == 1, ns))
+    assert out[0][single].isnan().all()
+    c.check(*c.run(pa=pa), "cut tiles")
+    out = c.run(pa=pa, with_lse=False)
+    c.check(out[0], None, "cut tiles, no log-sum-exp")
+
+
+def test_cut_prefill_tiles_captured():
+    c = Case(28, 4, 128, 16, [1, 40], [600, 1090], seed=12)
+    g, pa = c.gpu(), c.plan()
+    ref = c.run(g=g, pa=pa)
+    out, lse = pa.alloc_out(g["q"], True)
+    args = pa.kv8_args(g["q"], g["k"], g["v"], g["s"], g["bt"], g["ls"], g["qsl"], out, lse)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        F.flex_attn_mixed_kv8(pa.plan, args, F.FLEX_MODE_SERIAL)
+    for k in range(3):
+        out.zero_()
+        lse.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out.cpu().view(torch.int16), ref[0].view(torch.int16)) and torch.equal(lse.cpu(), ref[1]), f"replay {k}"
+    c.check(*ref, "captured")
+
+
+@pytest.mark.parametrize("hq,hkv,d,P", [(28, 4, 128, 16), (28, 4, 128, 64), (32, 8, 64, 16), (4, 4, 64, 64)])
+def test_key_tiles_in_two_groups(hq, hkv, d, P):
+    """Work-groups of two key groups: odd and even counts of key tiles, rows
+    whose keys all lie in the first group's, a tile with nothing for the second."""
+    ns, ls = [2, 3, 31, 33, 64, 100, 20, 2], [2, 40, 31, 97, 64, 290, 257, 33]
+    c = Case(hq, hkv, d, P, ns, ls, seed=hq + d, spread=6)
+    pa = c.plan(cus_decode=0)
+    i = pa.plan.info
+    assert i["n_prefill_items"] * i["prefill_grid_y"] <= i["cus_prefill"]
+    c.check(*c.run("prefill", pa=pa), "two groups")
+
+
 def test_prefill_crosses_a_block_table_window():
     """Page 16: 512 block-table entries cover 8192 keys; the chunk ends past that."""
     c = Case(4, 1, 64, 16, [70, 1], [8230, 9000], seed=9)

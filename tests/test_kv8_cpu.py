@@ -113,6 +113,32 @@ def test_plans_for_8_bit_caches_match_the_rederivation():
                             bm=rng.choice([0, 128]), decode_tail=rng.choice([0, -1])), qsl, ls, maxp)
 
 
+@pytest.mark.parametrize("n,ls,cut", [((64,), (4000,), True), ((2,), (300,), False), ((2,), (448,), False), ((2,), (449,), True), ((64, 3), (64, 2500), True),
+                                      ((64, 1, 200), (4000, 900, 210), True), ((3000,), (3000,), False), ((200,) * 5, (3000,) * 5, False)])
+def test_few_prefill_tiles_are_cut_along_their_keys(n, ls, cut):
+    """Pieces of a tile are disjoint, in order and cover its keys; slots are
+    those of the workspace, one after another; work-groups stay within the units."""
+    sh = GQA[0]
+    qsl = np.concatenate([[0], np.cumsum(n)]).astype(int).tolist()
+    maxp = max(-(-x // sh.page_size) for x in ls)
+    compare(sh, OP.Opts(kv_bits=8), qsl, list(ls), maxp)
+    p = F.flex_attn_plan(F.make_shape(sh.num_q_heads, sh.num_kv_heads, sh.head_dim_qk, sh.head_dim_v, sh.page_size, sh.sm_scale),
+                         F.make_opts(kv_bits=8), qsl, list(ls), maxp)
+    info, w = p.info, list(p.export())
+    items = [w[w[10] + 8 * i:w[10] + 8 * i + 8] for i in range(info["n_prefill_items"])]   # w[10]: where they start
+    pieces = [it for it in items if it[6] > 1]
+    assert bool(pieces) == cut
+    if not cut:
+        return
+    assert info["workspace_bytes"] > 0 and len(items) * info["prefill_grid_y"] <= info["cus_prefill"]
+    for tile in {tuple(it[:4]) for it in pieces}:
+        own = sorted((it for it in pieces if tuple(it[:4]) == tile), key=lambda it: it[5])
+        s, _, _, r1 = tile
+        assert own[0][5] == 0 and own[-1][4] == ls[s] - n[s] + (r1 - 1) // 7 + 1 and own[0][6] == len(own)
+        assert all(a[4] == b[5] and a[4] % 64 == 0 and a[7] + 1 == b[7] for a, b in zip(own, own[1:]))
+    assert sorted(it[7] for it in pieces) == list(range(len(pieces)))
+
+
 @pytest.mark.parametrize("sh,opts", [
     (GQA[0], OP.Opts(kv_bits=4)), (GQA[0], OP.Opts(kv_bits=-8)), (GQA[0], OP.Opts(kv_bits=8, bm=32)),
     (GQA[0], OP.Opts(kv_bits=8, bm=16)), (OP.Shape(128, 1, 576, 512, 64, 0.07, 1), OP.Opts(kv_bits=8)),
