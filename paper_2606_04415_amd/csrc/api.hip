@@ -222,8 +222,7 @@ int run_prefill(const flex_attn_plan_t* plan, AttnParams p, const flex_attn_args
   p.items = static_cast<const int32_t*>(a->d_plan) + plan->words[H_OFF_PRE];
   p.n_items = info.n_prefill_items;
   p.grid_y = info.prefill_grid_y;
-  p.n_cus = info.cus_prefill;
-  p.longest_prefill = plan->longest_prefill;
+  p.key_groups = plan->key_groups;
   p.n_cut_tiles = plan->n_cut_tiles;
   p.cut_tiles = static_cast<const int32_t*>(a->d_plan) + plan->words[H_OFF_FUSED] + plan->words[H_N_FUSED];
   const hipError_t e = launch_prefill(p, plan->shape.head_dim_qk, info.bm, s);

@@ -1765,13 +1765,8 @@ static hipError_t launch_flat_t(const AttnParams& p, dim3 grid, hipStream_t stre
 template <int D, int P>
 static hipError_t launch_prefill_flat(const AttnParams& p, int bm, dim3 grid, hipStream_t stream) {
   if (bm == 128 && p.kv_scales) {
-    // Two key groups where work-groups have a compute unit each to themselves
-    // and tiles to share (28/4 heads of 128, one group against two: a prompt of
-    // 512 22.9 and 19.4 us, of 1024 on 4000 keys 155 and 107, but of 64 8.4 and
-    // 9.3, and 8 of 256, 448 work-groups, 17.8 and 23.0).
-    const bool pairs = int64_t(p.n_items) * p.grid_y <= p.n_cus && p.longest_prefill >= 256;
-    const hipError_t e = pairs ? launch_flat_t<D, 4, 2, 32, P, 2, 2, 2>(p, grid, stream)
-                               : launch_flat_t<D, 4, 2, 32, P, 2, 3, 1>(p, grid, stream);
+    const hipError_t e = p.key_groups == 2 ? launch_flat_t<D, 4, 2, 32, P, 2, 2, 2>(p, grid, stream)
+                                           : launch_flat_t<D, 4, 2, 32, P, 2, 3, 1>(p, grid, stream);
     return e != hipSuccess || p.n_cut_tiles == 0 ? e : launch_merge_tiles(p, D, stream);
   }
   if (bm == 128) return launch_flat_t<D, 4, 2, 32, P, 3, 3>(p, grid, stream);

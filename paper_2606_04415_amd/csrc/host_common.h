@@ -127,7 +127,7 @@ struct flex_attn_plan {
   size_t pre_ws_offset;     // 8-bit caches: bytes of the workspace before the prefill pieces' part
   int32_t n_pre_pieces;     // pieces of cut prefill tiles
   int32_t n_cut_tiles;      // cut prefill tiles
-  int32_t longest_prefill;  // most keys of a prefill item
+  int32_t key_groups;       // 8-bit caches: of a prefill work-group
   std::vector<int32_t> words;
 };
 

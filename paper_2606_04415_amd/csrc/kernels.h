@@ -43,8 +43,7 @@ struct AttnParams {
   float* pre_o;               // [slot][kv head][128][d_v] unnormalised partial outputs
   const int32_t* cut_tiles;   // item of the first piece of every cut tile
   int32_t n_cut_tiles;        // 0: no tile is cut
-  int32_t n_cus;              // prefill: compute units of its share
-  int32_t longest_prefill;    // most keys of an item
+  int32_t key_groups;         // of a prefill work-group
 };
 
 // Allow a kernel the dynamic LDS it launches with. The attribute is set on

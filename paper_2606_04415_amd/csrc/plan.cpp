@@ -571,8 +571,22 @@ extern "C" int flex_attn_plan(const flex_attn_shape* shape, const flex_attn_plan
   // Behind it, per (piece of a cut prefill tile, KV head) the same of its 128 rows.
   plan->pre_ws_offset = size_t(cdiv(int64_t(ws), 256) * 256);
   plan->n_pre_pieces = n_pre_pieces;
-  plan->longest_prefill = 0;
-  for (const Tile& t : tiles) plan->longest_prefill = std::max(plan->longest_prefill, t.kend - t.kbeg);
+  // Two key groups a work-group where the longest item's keys exceed what a
+  // compute unit has to do on average (half of that more for heads of 64, of
+  // which a unit holds twice the work-groups), and it has enough of them to
+  // share. One group and two, 28/4 heads of 128, us: a prompt of 512 22.9 and
+  // 19.4, of 2048 73.6 and 56.3, of 1024 on 4000 keys 155 and 107, two of 1024
+  // 42.8 and 37.9; but one of 64 8.4 and 9.3, 8 of 256 17.8 and 23.0, 4 of 512
+  // on 500 43.8 and 49.6, one of 4096 150 and 182. 32/8 of 64: 2048 50.0 and
+  // 39.3, 1536 on 4000 130 and 110; two of 1500 40.4 and 41.5.
+  int64_t longest_item = 0, all_keys = 0;
+  for (const Tile& t : tiles) {
+    longest_item = std::max<int64_t>(longest_item, t.kend - t.kbeg);
+    all_keys += t.kend - t.kbeg;
+  }
+  const bool own_unit = int64_t(tiles.size()) * sh.num_kv_heads <= cus_prefill;
+  plan->key_groups = 2 * all_keys * sh.num_kv_heads <= (sh.head_dim_qk == 64 ? 3 : 2) * longest_item * cus_prefill &&
+                     longest_item >= (own_unit ? 256 : 512) ? 2 : 1;
   if (n_pre_pieces > 0) ws = plan->pre_ws_offset + size_t(n_pre_pieces) * sh.num_kv_heads * 128 * (2 + sh.head_dim_v) * 4;
   flex_attn_plan_info& info = plan->info;
   std::memset(&info, 0, sizeof(info));
