@@ -17,7 +17,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG, "csrc")
 ROOT = os.path.dirname(PKG)
 LIB = os.path.join(PKG, "libflexattn.so")
-SOURCES = ["attention.hip", "decode_kv8.hip", "latent.hip", "kv_append.hip", "api.hip", "plan.cpp", "controller.cpp"]
+SOURCES = ["attention.hip", "decode_kv8.hip", "prefill_kv8.hip", "latent.hip", "kv_append.hip", "api.hip", "plan.cpp", "controller.cpp"]
 # sources whose values may be NaN: what they copy or quantise is the caller's
 KEEPS_NANS = {"kv_append.hip"}
 ARCH = "gfx950"

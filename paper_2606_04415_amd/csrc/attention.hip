@@ -510,30 +510,6 @@ __device__ __forceinline__ void dma16(const void* src, void* lds_wave_base) {
   asm volatile("global_load_lds_dwordx4 %0, off" ::"v"(src), "{m0}"(__builtin_amdgcn_readfirstlane(m0)) : "memory");
 }
 
-// 16-byte buffer -> LDS copy per lane: lane i writes lds_wave_base + 16 i,
-// reading rsrc base + voffset. The resource (page base, in SGPRs) is
-// wave-uniform and the per-lane offset fixed for the launch, so a tile's
-// loads cost scalar work only. Inline assembly for the same reason as dma16.
-// The resource words often come straight from v_readfirstlane: a vector
-// instruction writing an SGPR that a vector-memory instruction then reads
-// needs 5 wait states, and the compiler's hazard check does not look inside
-// inline assembly, so the block opens with them (s_nop 5: 6 wait states,
-// which also covers the M0 write before an LDS DMA).
-__device__ __forceinline__ void dma16_buf(const i32x4& rsrc, uint32_t voffset, void* lds_wave_base) {
-  const uint32_t m0 = uint32_t(reinterpret_cast<uintptr_t>((lds_byte_ptr)(lds_wave_base)));
-  asm volatile("s_nop 5\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(voffset), "s"(rsrc),
-               "{m0}"(__builtin_amdgcn_readfirstlane(m0))
-               : "memory");
-}
-
-// Raw buffer resource over [base, base + bytes) from a wave-uniform address.
-__device__ __forceinline__ i32x4 uniform_rsrc(const void* base, uint32_t bytes) {
-  const uint64_t a = reinterpret_cast<uint64_t>(base);
-  return i32x4{__builtin_amdgcn_readfirstlane(int32_t(uint32_t(a))),
-               __builtin_amdgcn_readfirstlane(int32_t(uint32_t(a >> 32) & 0xFFFFu)),
-               __builtin_amdgcn_readfirstlane(int32_t(bytes)), kBufferFlags};
-}
-
 template <int DQK, int DV, int NW, int RB, int BN, bool VALIAS, int NS>
 struct RowParCfg {
   static constexpr int DC = DQK / 32;
@@ -729,112 +705,10 @@ struct RowParLoader<true, DQK, DV, NW, BN, NS, P> : LatentLoader<P, false> {
   }
 };
 
-// Loader of tiles of 32 keys from an 8-bit cache, for work-groups of four
-// waves. Codes come by DMA into a ring of two raw tiles, and each wave converts
-// the part that it loaded into the bf16 tile of a stage (once for the
-// work-group; every wave's operand reads, of which each makes as many as the
-// tile holds, then see bf16). A load covers 64 16-byte chunks, whole rows of K
-// or of V, which all lie in one block of 16 keys: page, resource and scale are
-// wave-uniform. KG key groups of four waves have stages and raw tiles of their
-// own and one window of pages and scales between them.
-template <int D, int P, int KG>
-struct TileLoader8 {
-  using C = RowParCfg<D, D, 4, 1, 32, false, 2>;
-  static constexpr int CPR = D / 16;         // 16-byte chunks of codes in a row
-  static constexpr int RPL = 64 / CPR;       // rows of a load
-  static constexpr int NL = 2 * 32 * CPR / 256;   // loads of a wave per tile: K then V (head dim 128), or K or V (64)
-  static constexpr int RAW = 2 * 32 * D;     // bytes of a raw tile
-  static constexpr int WIN = P == 16 ? 512 : 256;   // block-table entries of a window
-  static constexpr int BPP = P / 16;         // blocks of a page
-  // LDS: each group's two stages and two raw tiles, the window's pages, its
-  // blocks' scale bytes; at the end, the states of all groups but the first.
-  static constexpr int REGION = 2 * C::STAGE + 2 * RAW, PT_OFF = KG * REGION, SC_OFF = PT_OFF + 4 * WIN;
-  static constexpr int STATE = 4 * 64 * (2 * D + 16);   // of a group: 2 row blocks' accumulators, maxima and sums
-  static constexpr size_t LDS_BYTES = std::max<size_t>(SC_OFF + 2 * WIN * BPP, (KG - 1) * STATE);
-
-  uint8_t* lds;                              // the group's region
-  const int* s_pt;
-  const uint16_t* s_sc;
-  const uint8_t* base[NL];
-  uint32_t sp[NL], ss[NL], ld_off[NL], st_off[NL][2];
-  int key_end, row0, lane, w;                // row0: first row of the wave's loads
-  bool is_v[NL];
-  u32x4 x[NL];                               // read_raw() to convert()
-  uint32_t scale;
-
-  __device__ __forceinline__ TileLoader8(const AttnParams& p, int head, uint8_t* lds_, const int*, int w_, int lane_,
-                                         int key_end_, int group)
-      : lds(lds_ + group * REGION), s_pt(reinterpret_cast<const int*>(lds_ + PT_OFF)),
-        s_sc(reinterpret_cast<const uint16_t*>(lds_ + SC_OFF)), key_end(key_end_), lane(lane_), w(w_) {
-    row0 = RPL * (w % (32 / RPL));
-    const int row = row0 + lane / CPR, c = lane % CPR;
-#pragma unroll
-    for (int j = 0; j < NL; ++j) {
-      is_v[j] = NL == 2 ? j == 1 : w >= 2;
-      const CacheRef& r = is_v[j] ? p.vc : p.kc;
-      base[j] = reinterpret_cast<const uint8_t*>(r.base) + int64_t(head) * r.sh;
-      sp[j] = uint32_t(r.sp);
-      ss[j] = uint32_t(r.ss);
-      ld_off[j] = uint32_t(lane / CPR) * ss[j] + 16u * uint32_t(lane % CPR);
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-        st_off[j][h] = is_v[j] ? uint32_t(C::V_OFF + row * C::CPRV * 16 + 16 * swz_v<D>(2 * c + h, row))
-                               : uint32_t(row * C::CPR * 16 + 16 * swz_k<D>(2 * c + h, row));
-    }
-  }
-  __device__ __forceinline__ uint8_t* raw(int slot, int j) const {
-    return lds + 2 * C::STAGE + slot * RAW + (w * NL + j) * 1024;
-  }
-  // Start the loads of the tile at kb into a raw slot. Rows past key_end repeat
-  // the last key's (masked later). (A tile starts on a multiple of 32 keys, so
-  // at page 16 the wave's first slot in its page is the same in every tile.)
-  __device__ __forceinline__ int first_page(int kb, int pt_base) const {   // of the wave's loads
-    return s_pt[uint32_t(min(kb + row0, key_end - 1)) / P - uint32_t(pt_base)];
-  }
-  __device__ __forceinline__ void fetch(int kb, int slot, int first) const {
-    const uint32_t page = uint32_t(__builtin_amdgcn_readfirstlane(first));
-    const bool whole = kb + row0 + RPL <= key_end;
-    const int key = min(kb + row0, key_end - 1);
-    const uint32_t in_page = P == 16 && whole ? uint32_t(row0) % 16 : uint32_t(key) % P;
-    i32x4 r[NL];
-#pragma unroll
-    for (int j = 0; j < NL; ++j)
-      r[j] = uniform_rsrc(base[j] + (uint64_t(page) * sp[j] + in_page * ss[j]), uint32_t(RPL) * ss[j]);
-    if (whole) {
-#pragma unroll
-      for (int j = 0; j < NL; ++j) dma16_buf(r[j], ld_off[j], raw(slot, j));
-    } else {
-      const uint32_t row = uint32_t(min(lane / CPR, key_end - 1 - key));
-#pragma unroll
-      for (int j = 0; j < NL; ++j) dma16_buf(r[j], row * ss[j] + 16u * uint32_t(lane % CPR), raw(slot, j));
-    }
-  }
-  // The wave's part of the raw tile at kb, whose loads have landed, into
-  // registers; then as bf16 into a stage.
-  __device__ __forceinline__ void read_raw(int kb, int slot, int pt_base) {
-    uint32_t block = uint32_t(min(kb + row0, key_end - 1)) / 16 - uint32_t(pt_base * BPP);
-    asm volatile("" : "+v"(block));   // read into a vector register: a scalar one would be waited for here
-    scale = s_sc[block];
-#pragma unroll
-    for (int j = 0; j < NL; ++j) x[j] = *reinterpret_cast<const u32x4*>(raw(slot, j) + 16 * lane);
-  }
-  __device__ __forceinline__ void convert(int st) const {
-    uint8_t* stage = lds + st * C::STAGE;
-#pragma unroll
-    for (int j = 0; j < NL; ++j) {
-      const float f = scale_of(is_v[j] ? scale >> 8 : scale);
-      *reinterpret_cast<u32x4*>(stage + st_off[j][0]) = codes_bf16x8(x[j][0], x[j][1], f, f);
-      *reinterpret_cast<u32x4*>(stage + st_off[j][1]) = codes_bf16x8(x[j][2], x[j][3], f, f);
-    }
-  }
-};
-
 // One work-group's work: item `item` of the phase, column `col`, threads
-// 0 .. NW*64-1 of the work-group, the work-group's dynamic LDS. KG > 0: an 8-bit
-// cache, and KG times NW waves, in groups that take every KG-th key tile.
-template <int DQK, int DV, int NW, int RB, int BN, bool VALIAS, int MODE, int P, int NS, int TB, int KG = 0>
+// 0 .. NW*64-1 of the work-group, the work-group's dynamic LDS.
+template <int DQK, int DV, int NW, int RB, int BN, bool VALIAS, int MODE, int P, int NS, int TB>
 __device__ __forceinline__ void rowpar_body(const AttnParams& p, int item, int col) {
-  constexpr bool KV8 = KG > 0;
   using C = RowParCfg<DQK, DV, NW, RB, BN, VALIAS, NS>;
   static_assert(NS >= 2 && NS <= 6, "stages");
   static_assert(BN % 32 == 0, "whole 32-key chunks per tile");
@@ -844,8 +718,7 @@ __device__ __forceinline__ void rowpar_body(const AttnParams& p, int item, int c
 
   const int tid = threadIdx.x;
   const int lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int w = KG > 1 ? wave % NW : wave, group = KG > 1 ? wave / NW : 0;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 15, gq = lane >> 4;
   const int32_t* it = p.items + 8 * (MODE == kDecodeLatent ? p.order[item] : item);
   const int seq = it[0];
@@ -894,7 +767,7 @@ __device__ __forceinline__ void rowpar_body(const AttnParams& p, int item, int c
     wave_full = L - nq + wr0 + 1;
   } else if constexpr (MODE == kPrefillFlat) {
     const int r0 = it[2], r1 = it[3];
-    key_begin = KV8 ? it[5] : 0;
+    key_begin = 0;
     key_end = it[4];
     head_kv = col;
     const int G = p.G;
@@ -952,10 +825,8 @@ __device__ __forceinline__ void rowpar_body(const AttnParams& p, int item, int c
   // latent rows, whose operands fill the register file, as one partial per
   // lane on the VALU (lpart, row n, this lane's keys; summed over the four
   // lane groups at the end). Both add the bf16-rounded probabilities that
-  // feed the P x V product. Over an 8-bit cache the VALU adds the
-  // probabilities before they are rounded: the log-sum-exp is then good to
-  // fp32, and the outputs, whose roundings average out, as near as before.
-  constexpr bool kValuSum = VALIAS || KV8;
+  // feed the P x V product.
+  constexpr bool kValuSum = VALIAS;
   f32x4 o[RB][C::NACC], lsum[RB];
   float lpart[RB];
   // Row maxima start at the lowest finite float rather than -inf: -m then
@@ -972,14 +843,8 @@ __device__ __forceinline__ void rowpar_body(const AttnParams& p, int item, int c
   }
   const u32x4 ones = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};   // bf16 1.0 x 8
 
-  auto make_loader = [&] {
-    if constexpr (KV8) return TileLoader8<DQK, P, KG>(p, head_kv, lds, s_pt, w, lane, key_end, group);
-    else return RowParLoader<VALIAS, DQK, DV, NW, BN, NS, P>(p, head_kv, lds, s_pt, w, lane, key_end);
-  };
-  auto loader = make_loader();
-  auto issue = [&](int kb, int st, int pt_base) {
-    if constexpr (!KV8) loader.issue(kb, st, pt_base);
-  };
+  const RowParLoader<VALIAS, DQK, DV, NW, BN, NS, P> loader(p, head_kv, lds, s_pt, w, lane, key_end);
+  auto issue = [&](int kb, int st, int pt_base) { loader.issue(kb, st, pt_base); };
 
   // Per-lane LDS byte offsets of the MFMA operand reads within a stage. The
   // row swizzles depend only on the row modulo 16 (K) or 8 (V), so they are
@@ -1023,18 +888,13 @@ __device__ __forceinline__ void rowpar_body(const AttnParams& p, int item, int c
         reinterpret_cast<const uint16_t*>(base + ((32 * ch + 16 * half) * VROW + (VALIAS ? 32 * cv : 0))));
   };
 
-  auto none = [] {};
-  int region = 0;   // LDS offset of the wave's stages
-  if constexpr (KV8) region = group * TileLoader8<DQK, P, KG>::REGION;
-
   // One key tile: S^T = K Q^T per 32-key chunk, masking (only when the tile
   // crosses a row limit), the tile max of each row, lazy rescale, then
   // probabilities and O += P V, l += P 1 per chunk. (One instance per loop:
   // a masked and an unmasked copy in one loop body would be merged by the
   // compiler at a large register cost.)
-  // (scored() runs behind the scores' products, for work that hides there.)
-  auto compute_tile = [&](bool masked, int st, int kc0, auto&& scored) {
-    const uint8_t* stage = lds + __builtin_amdgcn_readfirstlane(st * C::STAGE + region);
+  auto compute_tile = [&](bool masked, int st, int kc0) {
+    const uint8_t* stage = lds + __builtin_amdgcn_readfirstlane(st * C::STAGE);
     f32x4 s[RB][2 * CH];
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb)
@@ -1079,8 +939,6 @@ __device__ __forceinline__ void rowpar_body(const AttnParams& p, int item, int c
       // read of the tile to the top would cost a register per value.
       __builtin_amdgcn_sched_barrier(0);
     }
-
-    scored();
 
     // s[rb][2ch + b][r] is the score of key kc0 + 32ch + 16b + 4gq + r for row n.
     float cmax[RB];
@@ -1141,11 +999,9 @@ __device__ __forceinline__ void rowpar_body(const AttnParams& p, int item, int c
         for (int e2 = 0; e2 < 4; ++e2) {
           const f32x4& sb = s[rb][2 * ch + (e2 >> 1)];
           const int r = 2 * (e2 & 1);
-          const float p0 = fast_exp2(fmaf(sb[r], p.scale_log2, neg_m));
-          const float p1 = fast_exp2(fmaf(sb[r + 1], p.scale_log2, neg_m));
-          pop[rb][e2] = pack_bf16x2(p0, p1);
-          if constexpr (KV8) lpart[rb] += p0 + p1;
-          else if constexpr (kValuSum)
+          pop[rb][e2] = pack_bf16x2(fast_exp2(fmaf(sb[r], p.scale_log2, neg_m)),
+                                    fast_exp2(fmaf(sb[r + 1], p.scale_log2, neg_m)));
+          if constexpr (kValuSum)
             lpart[rb] += __uint_as_float(pop[rb][e2] << 16) + __uint_as_float(pop[rb][e2] & 0xFFFF0000u);
         }
         if constexpr (!kValuSum) lsum[rb] = mfma_16x16x32(pop[rb], ones, lsum[rb]);
@@ -1193,107 +1049,10 @@ __device__ __forceinline__ void rowpar_body(const AttnParams& p, int item, int c
   // with tile kt - 1, so its stage takes tile kt + NS - 1) and computes.
   // Tiles that no row of the wave masks and that still have a tile to issue
   // after them run in a loop with fixed wait counts and no masking.
-  if constexpr (KV8) {
-    // Past the barrier of step kt (every wave has written its part of the
-    // group's tile and is done with the one before) the group's next tile is
-    // converted to where the last one was, between the parts of this one, and
-    // the loads of the third one on start into its raw slot; those of the
-    // second are in flight. The same windows of block-table entries as below,
-    // with the scales of their blocks.
-    using L8 = TileLoader8<DQK, P, KG>;
-    int* const pt = reinterpret_cast<int*>(lds + L8::PT_OFF);
-    uint16_t* const sc = reinterpret_cast<uint16_t*>(lds + L8::SC_OFF);
-    const int last = key_end > 0 ? (key_end - 1) / P : 0;
-    for (int wk0 = key_begin; wk0 < key_end; wk0 += L8::WIN * P) {
-      const int wk1 = min(key_end, wk0 + L8::WIN * P), pt_base = wk0 / P, tiles = (wk1 - wk0 + BN - 1) / BN;
-      const int pages = min(L8::WIN, last + 1 - pt_base);
-      const int ntiles = (tiles - group + KG - 1) / KG, steps = (tiles + KG - 1) / KG;   // the group's; the longest group's
-      auto key_of = [&](int kt) { return wk0 + (kt * KG + group) * BN; };
-      lds_barrier();
-      for (int i = tid; i < pages; i += KG * C::NT) pt[i] = bt_row[pt_base + i];
-      wait_vmem_all();
-      lds_barrier();
-      if (ntiles > 0) loader.fetch(key_of(0), 0, loader.first_page(key_of(0), pt_base));
-      if (ntiles > 1) loader.fetch(key_of(1), 1, loader.first_page(key_of(1), pt_base));
-      for (int i = tid; i < pages * L8::BPP; i += KG * C::NT)
-        sc[i] = *reinterpret_cast<const uint16_t*>(p.kv_scales + int64_t(pt[i / L8::BPP]) * p.scale_sp +
-                                                   (i % L8::BPP * p.Hkv + head_kv) * 2);
-      wait_vmem_all();
-      lds_barrier();
-      if (ntiles > 0) {
-        loader.read_raw(key_of(0), 0, pt_base);
-        loader.convert(0);
-      }
-      if (ntiles > 2) loader.fetch(key_of(2), 0, loader.first_page(key_of(2), pt_base));
-      // Tiles that no row of the wave masks.
-      const int steady = wave_on ? min(max(0, wave_full - wk0) / BN - group + KG - 1, tiles) / KG : 0;
-      int kt = 0;
-      for (; kt < min(steady, ntiles - 3); ++kt) {
-        lds_barrier();
-        wait_vmem<L8::NL>();
-        __atomic_signal_fence(__ATOMIC_SEQ_CST);   // the reads of the raw tile stay behind the wait
-        const int page = loader.first_page(key_of(kt + 3), pt_base);
-        loader.read_raw(key_of(kt + 1), (kt + 1) & 1, pt_base);
-        compute_tile(false, kt & 1, key_of(kt), [&] {
-          loader.convert((kt + 1) & 1);
-          loader.fetch(key_of(kt + 3), (kt + 1) & 1, page);
-        });
-      }
-      for (; kt < steps; ++kt) {
-        const int kc = key_of(kt);
-        lds_barrier();
-        if (kt + 1 < ntiles) {
-          if (kt + 2 < ntiles) wait_vmem<L8::NL>();
-          else wait_vmem<0>();
-          __atomic_signal_fence(__ATOMIC_SEQ_CST);
-          loader.read_raw(key_of(kt + 1), (kt + 1) & 1, pt_base);
-          loader.convert((kt + 1) & 1);
-          if (kt + 3 < ntiles) loader.fetch(key_of(kt + 3), (kt + 1) & 1, loader.first_page(key_of(kt + 3), pt_base));
-        }
-        if (kt < ntiles && wave_on && kc < wave_limit) compute_tile(kc + BN > wave_full, kt & 1, kc, none);
-      }
-    }
-    // The groups' states meet in the first: row maxima and sums, accumulators
-    // scaled to the common maximum, in group order.
-    if constexpr (KG > 1) {
-      static_assert(RB == 2, "the state holds two row blocks");
-      lds_barrier();
-      auto state = [&](int g) { return lds + (g - 1) * L8::STATE + w * (L8::STATE / 4) + 16 * lane; };
-      if (group > 0) {
-        uint8_t* at = state(group);
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-          for (int a = 0; a < C::NACC; ++a) *reinterpret_cast<f32x4*>(at + (rb * C::NACC + a) * 1024) = o[rb][a];
-        *reinterpret_cast<f32x4*>(at + RB * C::NACC * 1024) = f32x4{m[0], m[RB - 1], lpart[0], lpart[RB - 1]};
-      }
-      lds_barrier();
-      if (group > 0) return;
-#pragma unroll 1
-      for (int g = 1; g < KG; ++g) {
-        const uint8_t* at = state(g);
-        const f32x4 ml = *reinterpret_cast<const f32x4*>(at + RB * C::NACC * 1024);
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-          const float mg = ml[rb], M = fmaxf(m[rb], mg);
-          const float f0 = fast_exp2(m[rb] - M), f1 = fast_exp2(mg - M);
-          m[rb] = M;
-          lpart[rb] = lpart[rb] * f0 + ml[2 + rb] * f1;
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const float a0 = shfl_f(f0, 4 * gq + r), a1 = shfl_f(f1, 4 * gq + r);
-#pragma unroll
-            for (int a = 0; a < C::NACC; ++a)
-              o[rb][a][r] = o[rb][a][r] * a0 + reinterpret_cast<const float*>(at + (rb * C::NACC + a) * 1024)[r] * a1;
-          }
-        }
-      }
-    }
-  }
   constexpr int WIN_KEYS = kPageWin * P;
   static_assert(WIN_KEYS % BN == 0, "windows hold whole tiles");
   const int last_page = key_end > 0 ? (key_end - 1) / P : 0;
-  for (int wk0 = key_begin; !KV8 && wk0 < key_end; wk0 += WIN_KEYS) {
+  for (int wk0 = key_begin; wk0 < key_end; wk0 += WIN_KEYS) {
     const int wk1 = min(key_end, wk0 + WIN_KEYS);
     const int pt_base = wk0 / P;
     lds_barrier();
@@ -1316,7 +1075,7 @@ __device__ __forceinline__ void rowpar_body(const AttnParams& p, int item, int c
       wait_vmem<(NS - 2) * C::NI>();
       lds_barrier();
       issue(wk0 + (kt + NS - 1) * BN, (kt + NS - 1) % NS, pt_base);
-      compute_tile(false, kt % NS, wk0 + kt * BN, none);
+      compute_tile(false, kt % NS, wk0 + kt * BN);
     }
     for (; kt < ntiles; ++kt) {
       const int kc = wk0 + kt * BN;
@@ -1324,7 +1083,7 @@ __device__ __forceinline__ void rowpar_body(const AttnParams& p, int item, int c
       lds_barrier();
       if (kt + NS - 1 < ntiles) issue(wk0 + (kt + NS - 1) * BN, (kt + NS - 1) % NS, pt_base);
       if (!wave_on || kc >= wave_limit) continue;   // past this wave's rows: loads and barriers only
-      compute_tile(kc + BN > wave_full, kt % NS, kc, none);
+      compute_tile(kc + BN > wave_full, kt % NS, kc);
     }
   }
 
@@ -1337,28 +1096,6 @@ __device__ __forceinline__ void rowpar_body(const AttnParams& p, int item, int c
   if constexpr (MODE != kDecodeLatent) {
     if (!wave_on) return;
     const int r0 = it[2], r1 = it[3];
-    if constexpr (KV8) {
-      if (it[6] > 1) {   // a piece of the tile's keys: its state, for the merge
-        const int64_t row0 = (int64_t(it[7]) * p.Hkv + head_kv) * 128;
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int i = (w * RB + rb) * 16 + 4 * gq + r;
-            const float mr = shfl_f(m[rb], 4 * gq + r), lr = shfl_f(ltot[rb], 4 * gq + r);
-            if (r0 + i >= r1) continue;
-            float* dst = p.pre_o + (row0 + i) * DV + n;
-#pragma unroll
-            for (int cv = 0; cv < C::NACC; ++cv) dst[16 * cv] = o[rb][cv][r];
-            if (n == 0) {
-              p.pre_stats[(row0 + i) * 2] = mr;
-              p.pre_stats[(row0 + i) * 2 + 1] = lr;
-            }
-          }
-        }
-        return;
-      }
-    }
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
       const int blk = MODE == kPrefillGrouped ? ((w % TB) * RB + rb) : (w * RB + rb);
@@ -1451,8 +1188,8 @@ void rowpar_kernel(AttnParams p) {
 // per SIMD are the register budget the compiler is held to, so that
 // 4 * WPE / NW work-groups share a compute unit and their barriers drift
 // apart. 1-D XCD-aware grid as for kPrefillGrouped.
-template <int D, int NW, int RB, int BN, int P, int NS, int WPE, int KG = 0>
-__global__ __launch_bounds__(NW * 64 * (KG > 1 ? KG : 1)) __attribute__((amdgpu_waves_per_eu(WPE)))
+template <int D, int NW, int RB, int BN, int P, int NS, int WPE>
+__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(WPE)))
 void flat_prefill_kernel(AttnParams p) {
   int item = int(blockIdx.x), col = int(blockIdx.y);
   if (p.xcd_remap) {
@@ -1461,7 +1198,7 @@ void flat_prefill_kernel(AttnParams p) {
     item = j * (8 / p.grid_y) + x / p.grid_y;
     if (item >= p.n_items) return;
   }
-  rowpar_body<D, D, NW, RB, BN, false, kPrefillFlat, P, NS, 1, KG>(p, item, col);
+  rowpar_body<D, D, NW, RB, BN, false, kPrefillFlat, P, NS, 1>(p, item, col);
 }
 
 // Per-head prefill with split-out heads (keys 192, values 128): tiles of 128
@@ -1745,15 +1482,13 @@ static hipError_t launch_perhead_t(const AttnParams& p, dim3 grid, hipStream_t s
   return hipGetLastError();
 }
 
-template <int D, int NW, int RB, int BN, int P, int NS, int WPE, int KG = 0>
+template <int D, int NW, int RB, int BN, int P, int NS, int WPE>
 static hipError_t launch_flat_t(const AttnParams& p, dim3 grid, hipStream_t stream) {
   using C = RowParCfg<D, D, NW, RB, BN, false, NS>;
-  size_t lds = C::LDS_BYTES;
-  if constexpr (KG > 0) lds = TileLoader8<D, P, KG>::LDS_BYTES;
-  auto kern = flat_prefill_kernel<D, NW, RB, BN, P, NS, WPE, KG>;
-  const hipError_t attr = set_dynamic_lds(reinterpret_cast<const void*>(kern), lds);
+  auto kern = flat_prefill_kernel<D, NW, RB, BN, P, NS, WPE>;
+  const hipError_t attr = set_dynamic_lds(reinterpret_cast<const void*>(kern), C::LDS_BYTES);
   if (attr != hipSuccess) return attr;
-  hipLaunchKernelGGL(kern, grid, dim3(C::NT * (KG > 1 ? KG : 1)), lds, stream, p);
+  hipLaunchKernelGGL(kern, grid, dim3(C::NT), C::LDS_BYTES, stream, p);
   return hipGetLastError();
 }
 
@@ -1764,11 +1499,6 @@ static hipError_t launch_flat_t(const AttnParams& p, dim3 grid, hipStream_t stre
 // compute unit and their barriers drift apart.
 template <int D, int P>
 static hipError_t launch_prefill_flat(const AttnParams& p, int bm, dim3 grid, hipStream_t stream) {
-  if (bm == 128 && p.kv_scales) {
-    const hipError_t e = p.key_groups == 2 ? launch_flat_t<D, 4, 2, 32, P, 2, 2, 2>(p, grid, stream)
-                                           : launch_flat_t<D, 4, 2, 32, P, 2, 3, 1>(p, grid, stream);
-    return e != hipSuccess || p.n_cut_tiles == 0 ? e : launch_merge_tiles(p, D, stream);
-  }
   if (bm == 128) return launch_flat_t<D, 4, 2, 32, P, 3, 3>(p, grid, stream);
   return hipErrorInvalidValue;
 }
@@ -1824,6 +1554,7 @@ static hipError_t launch_prefill_p(const AttnParams& p, int dqk, int bm, dim3 gr
 
 hipError_t launch_prefill(const AttnParams& p, int dqk, int bm, hipStream_t stream) {
   if (p.n_items == 0) return hipSuccess;
+  if (p.kv_scales) return launch_prefill_kv8(p, dqk, stream);
   const dim3 grid(p.n_items, p.grid_y);
   if (p.P == 16) return launch_prefill_p<16>(p, dqk, bm, grid, stream);
   if (p.P == 64) return launch_prefill_p<64>(p, dqk, bm, grid, stream);

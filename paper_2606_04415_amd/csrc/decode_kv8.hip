@@ -439,52 +439,6 @@ __global__ __launch_bounds__(256) void merge_many_kernel(AttnParams p) {
   if (c == 0 && p.lse) p.lse[row] = (top + log2f(den)) * kLn2;
 }
 
-// Joins the pieces of a prefill tile whose keys were cut: work-group (cut tile,
-// KV head, slice of 8 or 16 rows), a thread per four columns of a row, the
-// pieces in order, four loads in flight. A piece in which a row sees no key
-// holds a sum of 0 and the lowest maximum, which weighs 0: every row sees key 0.
-template <int DV>
-__global__ __launch_bounds__(256) void merge_tiles_kernel(AttnParams p) {
-  constexpr int CT = DV / 4, RPW = 256 / CT, KB = 4;
-  const int32_t* it = p.items + 8 * p.cut_tiles[blockIdx.x];
-  const int pieces = it[6], h = blockIdx.y;
-  const int c = threadIdx.x % CT, i = blockIdx.z * RPW + threadIdx.x / CT, r = it[2] + i;
-  if (r >= it[3]) return;
-  const int64_t step = int64_t(p.Hkv) * 128, row0 = (int64_t(it[7]) * p.Hkv + h) * 128 + i;
-  float M = -INFINITY, den = 0.f;
-  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  for (int j0 = 0; j0 < pieces; j0 += KB) {
-    float mj[KB], lj[KB];
-    f32x4 vj[KB];
-#pragma unroll
-    for (int k = 0; k < KB; ++k) {
-      const int64_t at = row0 + min(j0 + k, pieces - 1) * step;
-      mj[k] = j0 + k < pieces ? p.pre_stats[at * 2] : -INFINITY;
-      lj[k] = p.pre_stats[at * 2 + 1];
-      vj[k] = *reinterpret_cast<const f32x4*>(p.pre_o + at * DV + 4 * c);
-    }
-    float Mn = M;
-#pragma unroll
-    for (int k = 0; k < KB; ++k) Mn = fmaxf(Mn, mj[k]);
-    const float sc = M == -INFINITY ? 0.f : fast_exp2(M - Mn);
-    den *= sc;
-    acc *= sc;
-    M = Mn;
-#pragma unroll
-    for (int k = 0; k < KB; ++k) {
-      const float f = mj[k] == -INFINITY ? 0.f : fast_exp2(mj[k] - M);
-      den += f * lj[k];
-      acc += f * vj[k];
-    }
-  }
-  const float inv = 1.f / den;
-  const int tok = r / p.G;
-  const int64_t row = int64_t(p.qsl[it[0]] + tok) * p.Hq + h * p.G + (r - tok * p.G);
-  *reinterpret_cast<u32x2*>(p.out + row * DV + 4 * c) =
-      u32x2{pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv)};
-  if (c == 0 && p.lse) p.lse[row] = (M + log2f(den)) * kLn2;
-}
-
 template <int D, int P>
 hipError_t launch_t(const AttnParams& p, hipStream_t stream) {
   const dim3 grid(p.n_ranges, p.grid_y);
@@ -504,13 +458,6 @@ hipError_t launch_t(const AttnParams& p, hipStream_t stream) {
 }
 
 }  // namespace
-
-hipError_t launch_merge_tiles(const AttnParams& p, int head_dim, hipStream_t stream) {
-  if (head_dim == 128) hipLaunchKernelGGL(merge_tiles_kernel<128>, dim3(p.n_cut_tiles, p.Hkv, 16), dim3(256), 0, stream, p);
-  else if (head_dim == 64) hipLaunchKernelGGL(merge_tiles_kernel<64>, dim3(p.n_cut_tiles, p.Hkv, 8), dim3(256), 0, stream, p);
-  else return hipErrorInvalidValue;
-  return hipGetLastError();
-}
 
 hipError_t launch_merge_many(const AttnParams& p, int head_dim, hipStream_t stream) {
   const dim3 grid(p.n_merge, p.grid_y, p.rows_per_wg);

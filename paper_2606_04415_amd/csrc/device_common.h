@@ -18,6 +18,8 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) uint8_t* lds_byte_ptr;
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -83,6 +85,33 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
 // Word 3 of a raw (unswizzled, stride 0) buffer resource on gfx9: 32-bit
 // data format, so out-of-range dword loads return zero.
 constexpr int kBufferFlags = 0x00020000;
+
+// 16-byte buffer -> LDS copy per lane: lane i writes lds_wave_base + 16 i,
+// reading rsrc base + voffset. The resource (page base, in SGPRs) is
+// wave-uniform and the per-lane offset fixed for the launch, so a tile's
+// loads cost scalar work only. Inline assembly so that the compiler's wait
+// insertion does not see an LDS write in flight: it would drain every
+// outstanding load before LDS reads it cannot prove disjoint. Completion is
+// awaited explicitly (wait_vmem).
+// The resource words often come straight from v_readfirstlane: a vector
+// instruction writing an SGPR that a vector-memory instruction then reads
+// needs 5 wait states, and the compiler's hazard check does not look inside
+// inline assembly, so the block opens with them (s_nop 5: 6 wait states,
+// which also covers the M0 write before an LDS DMA).
+__device__ __forceinline__ void dma16_buf(const i32x4& rsrc, uint32_t voffset, void* lds_wave_base) {
+  const uint32_t m0 = uint32_t(reinterpret_cast<uintptr_t>((lds_byte_ptr)(lds_wave_base)));
+  asm volatile("s_nop 5\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(voffset), "s"(rsrc),
+               "{m0}"(__builtin_amdgcn_readfirstlane(m0))
+               : "memory");
+}
+
+// Raw buffer resource over [base, base + bytes) from a wave-uniform address.
+__device__ __forceinline__ i32x4 uniform_rsrc(const void* base, uint32_t bytes) {
+  const uint64_t a = reinterpret_cast<uint64_t>(base);
+  return i32x4{__builtin_amdgcn_readfirstlane(int32_t(uint32_t(a))),
+               __builtin_amdgcn_readfirstlane(int32_t(uint32_t(a >> 32) & 0xFFFFu)),
+               __builtin_amdgcn_readfirstlane(int32_t(bytes)), kBufferFlags};
+}
 
 // Element offset of (page, slot, head) in a paged cache with element strides.
 struct PagedCache {

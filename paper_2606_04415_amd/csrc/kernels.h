@@ -58,8 +58,9 @@ hipError_t launch_decode(const AttnParams& p, int head_dim_qk, bool has_splits, 
 hipError_t launch_decode_merge(const AttnParams& p, int head_dim_qk, hipStream_t stream);
 // Grouped-query decode over an 8-bit cache, without the merge (decode_kv8.hip).
 hipError_t launch_decode_kv8(const AttnParams& p, int head_dim, hipStream_t stream);
-// Joins the pieces of cut prefill tiles.
-hipError_t launch_merge_tiles(const AttnParams& p, int head_dim, hipStream_t stream);
+// Grouped-query prefill over an 8-bit cache, the merge of cut tiles included
+// (prefill_kv8.hip).
+hipError_t launch_prefill_kv8(const AttnParams& p, int head_dim, hipStream_t stream);
 hipError_t launch_merge_many(const AttnParams& p, int head_dim, hipStream_t stream);
 // Latent rows in groups of 128 (latent.hip).
 hipError_t launch_latent128(const AttnParams& p, bool decode, dim3 grid, hipStream_t stream);

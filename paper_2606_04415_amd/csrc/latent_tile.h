@@ -14,9 +14,6 @@
 
 namespace flexattn {
 
-typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) uint8_t* lds_byte_ptr;
-
 constexpr int kLatentQK = 576, kLatentV = 512;
 constexpr int kLatentBN = 32;                                  // keys of a tile
 constexpr int kLatentRow = 1056;                               // LDS bytes from row to row

@@ -23,7 +23,7 @@ import sys
 from collections import defaultdict
 
 KERNEL_SOURCES = tuple(os.path.join(os.path.dirname(os.path.abspath(__file__)), "csrc", f)
-                       for f in ("attention.hip", "decode_kv8.hip", "decode_walk.h", "latent.hip", "latent_tile.h",
+                       for f in ("attention.hip", "decode_kv8.hip", "decode_walk.h", "prefill_kv8.hip", "latent.hip", "latent_tile.h",
                                  "device_common.h"))
 COPY_BYTES = 1 << 30
 
