@@ -571,22 +571,28 @@ extern "C" int flex_attn_plan(const flex_attn_shape* shape, const flex_attn_plan
   // Behind it, per (piece of a cut prefill tile, KV head) the same of its 128 rows.
   plan->pre_ws_offset = size_t(cdiv(int64_t(ws), 256) * 256);
   plan->n_pre_pieces = n_pre_pieces;
-  // Two key groups a work-group where the longest item's keys exceed what a
-  // compute unit has to do on average (half of that more for heads of 64, of
-  // which a unit holds twice the work-groups), and it has enough of them to
-  // share. One group and two, 28/4 heads of 128, us: a prompt of 512 22.9 and
-  // 19.4, of 2048 73.6 and 56.3, of 1024 on 4000 keys 155 and 107, two of 1024
-  // 42.8 and 37.9; but one of 64 8.4 and 9.3, 8 of 256 17.8 and 23.0, 4 of 512
-  // on 500 43.8 and 49.6, one of 4096 150 and 182. 32/8 of 64: 2048 50.0 and
-  // 39.3, 1536 on 4000 130 and 110; two of 1500 40.4 and 41.5.
-  int64_t longest_item = 0, all_keys = 0;
-  for (const Tile& t : tiles) {
-    longest_item = std::max<int64_t>(longest_item, t.kend - t.kbeg);
-    all_keys += t.kend - t.kbeg;
+  // Two key groups a work-group where all of them run at once (a compute unit
+  // holds one of heads of 128, two of 64) and have enough keys to share, or
+  // where those that wait, which are the shortest, end no later than the
+  // longest. One group and two, 28/4 heads of 128, us: a prompt of 512 21.7 and
+  // 19.4, of 1024 on 4000 keys 143 and 110, of 2048 (448 work-groups) 67.9 and
+  // 57.2, two of 1024 40.7 and 37.6; but one of 64 8.1 and 9.3, 8 of 256 17.5
+  // and 22.9, 4 of 512 25.7 and 27.8, one of 2500 82.0 and 84.1, of 1200 on
+  // 4000 165 and 182. 32/8 heads of 64: 1024 on 4000 100 and 71, 2048 on 4096
+  // 136 and 124, 2500 56.3 and 48.3; 8 of 256 12.4 and 13.3, 2 of 1500 39.4 and
+  // 42.3.
+  plan->key_groups = 1;
+  if (kv8 && !tiles.empty()) {
+    const int64_t resident = sh.head_dim_qk == 64 ? 2 : 1;
+    const int64_t wgs = int64_t(tiles.size()) * sh.num_kv_heads, at_once = resident * cus_prefill;
+    auto keys = [&](int64_t wg) -> int64_t {   // of a work-group, the longest first
+      const Tile& t = tiles[wg / sh.num_kv_heads];
+      return t.kend - t.kbeg;
+    };
+    if (wgs <= at_once ? keys(0) >= (wgs <= cus_prefill ? 256 : 512)
+                       : resident * keys(0) >= 768 && resident * (keys(at_once - 1) + keys(at_once)) <= keys(0))
+      plan->key_groups = 2;
   }
-  const bool own_unit = int64_t(tiles.size()) * sh.num_kv_heads <= cus_prefill;
-  plan->key_groups = 2 * all_keys * sh.num_kv_heads <= (sh.head_dim_qk == 64 ? 3 : 2) * longest_item * cus_prefill &&
-                     longest_item >= (own_unit ? 256 : 512) ? 2 : 1;
   if (n_pre_pieces > 0) ws = plan->pre_ws_offset + size_t(n_pre_pieces) * sh.num_kv_heads * 128 * (2 + sh.head_dim_v) * 4;
   flex_attn_plan_info& info = plan->info;
   std::memset(&info, 0, sizeof(info));
