@@ -460,7 +460,8 @@ typedef struct flex_attn_rope {
  *  q        bf16 [n_tokens][Hq][d_qk]: token t's row starts at element
  *           t * q_stride; the Hq*d_qk values of a row are contiguous.
  *  q_out    bf16 [n_tokens][Hq][d_qk], contiguous. May be q itself when
- *           q_stride is Hq*d_qk; otherwise they must not overlap.
+ *           q_stride is Hq*d_qk; otherwise they must not overlap. It overlaps
+ *           nothing else that the call reads or writes.
  * Enqueues one kernel on stream and returns. */
 typedef struct flex_attn_rope_append_args {
   flex_attn_append_args kv;

@@ -495,6 +495,7 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(Kv8AppendParams p) {
   const int r0 = first & 15, rank = pos - first;
   const int64_t tf = t - rank;
   const int count = int(min(int64_t(16 - r0), q1 - tf));
+  if (count < 1) return;   // (query_start_loc out of order)
   const int64_t row0 = pos & (p.P - 1) & ~15;         // the block's first slot in its page
   const auto read = [&](auto& b, int h, int kv) {
     b.read(p, rope && !kv, (kv ? p.v_new : p.k_new) + h * D, kv ? p.v_new_stride : p.k_new_stride, tf, first, count, lane);

@@ -388,8 +388,12 @@ extern "C" int flex_attn_plan(const flex_attn_shape* shape, const flex_attn_plan
   // key_begin 0.)
   int32_t n_pre_pieces = 0;   // of cut tiles
   if (kv8 && !tiles.empty() && 2 * int64_t(tiles.size()) * sh.num_kv_heads <= cus_prefill) {
-    int64_t longest = 0, piece = kKv8MinPiece / kKv8PieceKeys;   // in units of kKv8PieceKeys
-    for (const Tile& t : tiles) longest = std::max(longest, cdiv(t.kend, kKv8PieceKeys));
+    int64_t longest = 0, total = 0;   // in units of kKv8PieceKeys
+    for (const Tile& t : tiles) {
+      longest = std::max(longest, cdiv(t.kend, kKv8PieceKeys));
+      total += cdiv(t.kend, kKv8PieceKeys);
+    }
+    int64_t piece = std::max(kKv8MinPiece / kKv8PieceKeys, cdiv(total * sh.num_kv_heads, cus_prefill));
     auto work_groups = [&] {
       int64_t n = 0;
       for (const Tile& t : tiles) n += cdiv(cdiv(t.kend, kKv8PieceKeys), piece);

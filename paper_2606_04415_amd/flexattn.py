@@ -313,7 +313,10 @@ def flex_attn_plan(shape: Shape, opts: Optional[PlanOpts], query_start_loc: Sequ
                               len(seq_lens), _i32_array(query_start_loc), _i32_array(seq_lens),
                               int(max_pages_per_seq), ctypes.byref(out))
     check(st, "flex_attn_plan")
-    return Plan(out.value)
+    plan = Plan(out.value)
+    plan.shape = Shape.from_buffer_copy(shape)
+    plan.batch = (len(seq_lens), int(query_start_loc[-1]))
+    return plan
 
 
 def plan_status(shape: Shape, opts: Optional[PlanOpts], query_start_loc, seq_lens, max_pages_per_seq) -> int:
@@ -638,7 +641,7 @@ def _check_kv8(k_cache, v_cache, kv_scales):
     _require(kv_scales.dtype == torch.float8_e8m0fnu, f"kv_scales must be float8_e8m0fnu, not {kv_scales.dtype}")
     _require(P % 16 == 0 and tuple(kv_scales.shape) == (pages, P // 16, heads, 2),
              f"kv_scales must be [{pages}, {P} / 16, {heads}, 2]")
-    _require(kv_scales[0].is_contiguous(), "kv_scales must be contiguous within a page")
+    _require(pages == 0 or kv_scales[0].is_contiguous(), "kv_scales must be contiguous within a page")
     return ks, vs, kv_scales.stride(0) if pages > 1 else P // 16 * heads * 2
 
 
@@ -699,18 +702,34 @@ def make_kv8_args(q, k_cache, v_cache, kv_scales, block_table, seq_lens, query_s
     a.attn.num_pages = k_cache.shape[0]
     a.kv_scales = kv_scales.data_ptr()
     a.device = _one_device([q, k_cache, v_cache, kv_scales, lse, d_plan, workspace])
+    _require(q.dim() == 3, "q must be [tokens, Hq, d]")
+    _require(out.shape[:2] == q.shape[:2] and out.shape[2:] == v_cache.shape[3:], "out must be [tokens, Hq, d]")
+    _require(lse is None or lse.shape == q.shape[:2], "lse must be [tokens, Hq]")
+    a.sizes = (q.shape[1], k_cache.shape[2], q.shape[2], v_cache.shape[3], k_cache.shape[1])
+    a.batch = (seq_lens.numel(), q.shape[0])
+    _require(block_table.shape[0] == a.batch[0] and query_start_loc.numel() == a.batch[0] + 1,
+             "block_table, seq_lens and query_start_loc must be of as many sequences")
     return a
 
 
+def _check_plan(plan, args):
+    _check_sizes(plan.shape, args)
+    if args.batch[0] != plan.batch[0] or args.batch[1] < plan.batch[1]:
+        raise ValueError(f"tensors of {args.batch[0]} sequences and {args.batch[1]} tokens, a plan for {plan.batch[0]} and {plan.batch[1]}")
+
+
 def flex_attn_decode_kv8(plan: Plan, args: Kv8Args, stream=None):
+    _check_plan(plan, args)
     _run("flex_attn_decode_kv8", args, stream, plan.handle, ctypes.byref(args))
 
 
 def flex_attn_prefill_kv8(plan: Plan, args: Kv8Args, stream=None):
+    _check_plan(plan, args)
     _run("flex_attn_prefill_kv8", args, stream, plan.handle, ctypes.byref(args))
 
 
 def flex_attn_mixed_kv8(plan: Plan, args: Kv8Args, mode: int, stream=None, corun: "Corun" = None):
+    _check_plan(plan, args)
     _run("flex_attn_mixed_kv8", args, stream, plan.handle, ctypes.byref(args), mode,
          last=(corun.handle if corun is not None else None,))
 

@@ -357,6 +357,13 @@ def test_binding_refuses_cpu_tensors_and_other_shapes():
                  lambda: F.flex_attn_mixed_kv8(plan, a, F.FLEX_MODE_SERIAL)):
         with pytest.raises(ValueError, match="GPU tensors"):
             call()
+    for p, match in ((F.flex_attn_plan(F.make_shape(28, 4, 128, 128, 64, 0.1), F.make_opts(kv_bits=8), [0, 1, 3], [40, 20], 3), "shape"),
+                     (F.flex_attn_plan(SHAPE, F.make_opts(kv_bits=8), [0, 1], [40], 3), "1 and 1"),
+                     (F.flex_attn_plan(SHAPE, F.make_opts(kv_bits=8), [0, 1, 4], [40, 20], 3), "2 and 4")):
+        for call in (lambda: F.flex_attn_decode_kv8(p, a), lambda: F.flex_attn_prefill_kv8(p, a),
+                     lambda: F.flex_attn_mixed_kv8(p, a, F.FLEX_MODE_SERIAL)):
+            with pytest.raises(ValueError, match=match):
+                call()
     kc = torch.zeros(4, 16, 4, 128, dtype=torch.bfloat16)
     slots, tab = torch.arange(3, dtype=torch.int32), F.rope_table(64, 128, device="cpu")
     pos = torch.zeros(3, dtype=torch.int32)
@@ -375,3 +382,9 @@ def test_binding_refuses_cpu_tensors_and_other_shapes():
         F.make_rope_append_args(t["q"], t["q_out"], t["k_new"], t["v_new"], slots[:2], kc, kc.clone())
     with pytest.raises(ValueError, match="bfloat16"):
         F.make_kv8_args(t["q"].float(), t["k"], t["v"], t["s"], t["bt"], t["ls"], t["qsl"], t["out"])
+    with pytest.raises(ValueError, match="out must"):
+        F.make_kv8_args(t["q"], t["k"], t["v"], t["s"], t["bt"], t["ls"], t["qsl"], t["out"][:2])
+    with pytest.raises(ValueError, match="lse must"):
+        F.make_kv8_args(t["q"], t["k"], t["v"], t["s"], t["bt"], t["ls"], t["qsl"], t["out"], torch.zeros(3, 27))
+    with pytest.raises(ValueError, match="as many sequences"):
+        F.make_kv8_args(t["q"], t["k"], t["v"], t["s"], t["bt"], t["ls"], t["qsl"][:2], t["out"])
