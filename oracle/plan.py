@@ -48,7 +48,8 @@ the contract is:
   F <= 3 * cus_prefill with cus_prefill < cus_total (a co-run share), else 32.
   Plans for 8-bit caches (kv_bits 8, grouped-query heads only) always take 128;
   their decode bytes count one byte a value and two scale bytes for each 16
-  tokens and KV head. With N tiles of U_i = ceil(key_end / 64) units, for at
+  tokens and KV head, and a decode work-group covers ceil(Hkv / C) KV heads, C =
+  ceil(Hkv * d / 512). With N tiles of U_i = ceil(key_end / 64) units, for at
   most half of the CUs (2 N * Hkv <= cus_prefill), and p >= 2 the least for
   which Hkv * sum ceil(U_i / p) <= cus_prefill: if (max U_i - p) * 64 >= 384, a
   tile is cut into n_i = ceil(U_i / p) pieces, the j-th over units
@@ -216,7 +217,8 @@ def build_plan(sh: Shape, opts: Optional[Opts], qsl: Sequence[int], seq_lens: Se
     if B > 0 and qsl[B] > 2**31 - 1:
         return PlanResult(ERR_INVALID_ARG)
 
-    heads_per_wg = min(sh.num_kv_heads, 8)
+    heads_per_wg = min(sh.num_kv_heads, 8) if o.kv_bits != 8 else \
+        cdiv(sh.num_kv_heads, cdiv(sh.num_kv_heads * sh.head_dim_qk, 512))
     mla_rows = MLA_ROWS_PER_WG_WIDE if sh.num_q_heads % MLA_ROWS_PER_WG_WIDE == 0 else MLA_ROWS_PER_WG
     W = (sh.num_q_heads // mla_rows) if mla else cdiv(sh.num_kv_heads, heads_per_wg)
     rows_per_wg = mla_rows if mla else heads_per_wg * (sh.num_q_heads // sh.num_kv_heads)

@@ -2,7 +2,7 @@
 // keys, KV head and K / V), grouped-query heads of 64 or 128.
 //
 // The work is laid out as for the bf16 cache: work-group (range r, column c)
-// owns one balanced page range and up to 8 KV heads, its waves walk the range
+// owns one balanced page range and some KV heads, its waves walk the range
 // as one stream of chunks with the next chunk's loads in flight, and a piece's
 // end writes an output or a partial. What differs:
 //
@@ -31,6 +31,7 @@ namespace flexattn {
 namespace {
 
 constexpr int kChunk = 64;                       // keys
+constexpr int kWaves = 4;                        // of a work-group (the planner gives it at most 4 * kRow bytes of a row)
 constexpr int kRow = 128;                        // bytes of a slot's row that a wave serves
 constexpr int kStage = 2 * kChunk * kRow;        // a wave's LDS buffer: K rows, then V rows
 constexpr int kOutRow = 132;                     // floats from row to row of outputs in the buffer
@@ -49,18 +50,18 @@ struct Chunk8 {
   uint32_t scales[2];       // lane l: scale bytes (K, V) of block l & 3, of the wave's heads
 };
 
-// One decode work-group's work, as decode_gqa_body. NW waves; COMBINE: several
-// of them serve the same heads.
-template <int D, int NW, int P, bool COMBINE>
-__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(NW / 4, 8)))
+// One decode work-group's work, as decode_gqa_body. COMBINE: several waves serve
+// the same heads.
+template <int D, int P, bool COMBINE>
+__global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(1, 8)))
 void decode_kv8_kernel(AttnParams p) {
   static_assert(D == 64 || D == 128, "head dim");
   constexpr int HPW = kRow / D;            // heads of a wave
   constexpr int DC = D / 32;               // 32-dim slices of a head's contraction
   constexpr int CBH = 8 / HPW;             // 16-column blocks of a head
   extern __shared__ __attribute__((aligned(16))) uint8_t s_dyn[];
-  __shared__ float s_m[COMBINE ? NW : 1][HPW][16], s_l[COMBINE ? NW : 1][HPW][16];
-  int* const s_pt = reinterpret_cast<int*>(s_dyn + NW * kStage);
+  __shared__ float s_m[COMBINE ? kWaves : 1][HPW][16], s_l[COMBINE ? kWaves : 1][HPW][16];
+  int* const s_pt = reinterpret_cast<int*>(s_dyn + kWaves * kStage);
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -69,7 +70,7 @@ void decode_kv8_kernel(AttnParams p) {
   const int G = p.G;
   const int HW = p.rows_per_wg / G;                  // KV heads of this work-group
   const int units = (HW + HPW - 1) / HPW;            // and the waves that serve them
-  const int WPH = COMBINE ? NW / units : 1;
+  const int WPH = COMBINE ? kWaves / units : 1;
   const int unit = w / WPH, u = w % WPH;
   const int g = col * HW + unit * HPW;               // this wave's first KV head
   const bool active = unit < units && g < p.Hkv;
@@ -113,7 +114,7 @@ void decode_kv8_kernel(AttnParams p) {
       const int k0 = scalar_word(p.items, 8 * i + 3), k1 = scalar_word(p.items, 8 * i + 4);
       const int32_t* bt_row = p.bt + int64_t(scalar_word(p.items, 8 * i)) * p.bt_stride + k0 / P;
       const int npg = pages_in(k0, k1, P);
-      for (int t = tid; t < npg; t += NW * 64) s_pt[poff + t] = bt_row[t];
+      for (int t = tid; t < npg; t += kWaves * 64) s_pt[poff + t] = bt_row[t];
       poff += npg;
     }
   }
@@ -313,7 +314,7 @@ void decode_kv8_kernel(AttnParams p) {
         }
       }
       lds_barrier();
-      for (int idx = tid; idx < units * G * 16; idx += NW * 64) {
+      for (int idx = tid; idx < units * G * 16; idx += kWaves * 64) {
         const int un = idx / (G * 16), row = idx / 16 % G, c = 8 * (idx % 16);
         const int e = c / D, head = col * HW + un * HPW + e;
         if (un * HPW + e >= HW || head >= p.Hkv) continue;
@@ -444,17 +445,15 @@ hipError_t launch_t(const AttnParams& p, hipStream_t stream) {
   const dim3 grid(p.n_ranges, p.grid_y);
   const size_t window = size_t(std::max(p.range_pages, 1)) * 4;
   const int hw = p.rows_per_wg / p.G, units = (hw * D + kRow - 1) / kRow;
-  auto go = [&](auto kern, int nw) {
-    const size_t lds = size_t(nw) * kStage + window;
+  auto go = [&](auto kern) {
+    const size_t lds = size_t(kWaves) * kStage + window;
     const hipError_t attr = set_dynamic_lds(reinterpret_cast<const void*>(kern), lds);
     if (attr != hipSuccess) return attr;
-    hipLaunchKernelGGL(kern, grid, dim3(nw * 64), lds, stream, p);
+    hipLaunchKernelGGL(kern, grid, dim3(kWaves * 64), lds, stream, p);
     return hipGetLastError();
   };
   // One wave per 128 bytes of a slot; when that is one or two, four share them.
-  if (units <= 2) return go(decode_kv8_kernel<D, 4, P, true>, 4);
-  if (units <= 4) return go(decode_kv8_kernel<D, 4, P, false>, 4);
-  return go(decode_kv8_kernel<D, 8, P, false>, 8);
+  return units <= 2 ? go(decode_kv8_kernel<D, P, true>) : go(decode_kv8_kernel<D, P, false>);
 }
 
 }  // namespace

@@ -72,6 +72,10 @@ constexpr int64_t kFlatResidentPerCu = 3;
 // KV heads one grouped-query decode work-group covers (one wave each, or
 // several waves per head when fewer heads than 4).
 constexpr int32_t kDecodeHeadsPerWG = 8;
+// Bytes of a slot's row that a decode work-group covers at most over an 8-bit
+// cache: 128 a wave. (Eight waves, whose registers spill, on the 8 heads of 128
+// of 64 sequences of 4000 keys: 105 us, 5.0 TB/s; two work-groups of four 88.)
+constexpr int64_t kKv8DecodeRow = 512;
 
 // Cost-model rates when the options leave them 0, measured on MI355X with
 // the Qwen2.5-7B-shaped mixed step: one CU's decode rate beside a running

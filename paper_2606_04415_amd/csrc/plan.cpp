@@ -181,7 +181,11 @@ extern "C" int flex_attn_plan(const flex_attn_shape* shape, const flex_attn_plan
   // spreads its stream over every memory channel); for the latent layout one
   // per 128 query heads (four waves of 32 heads share each key tile), or per
   // 64 (four of 16) when 128 does not divide Hq.
-  const int32_t heads_per_wg = std::min(sh.num_kv_heads, kDecodeHeadsPerWG);
+  // Over an 8-bit cache: as few groups of at most kKv8DecodeRow bytes of a
+  // slot's row as there can be, of sizes as even as they come.
+  const int32_t heads_per_wg =
+      kv8 ? int32_t(cdiv(sh.num_kv_heads, cdiv(int64_t(sh.num_kv_heads) * sh.head_dim_qk, kKv8DecodeRow)))
+          : std::min(sh.num_kv_heads, kDecodeHeadsPerWG);
   const int32_t latent_rows = sh.num_q_heads % kLatentRowsPerWGWide == 0 ? kLatentRowsPerWGWide : kLatentRowsPerWG;
   const int32_t W = latent ? sh.num_q_heads / latent_rows : int32_t(cdiv(sh.num_kv_heads, heads_per_wg));
   // Prefill work-groups per tile: one per query head (latent layout), or one per
