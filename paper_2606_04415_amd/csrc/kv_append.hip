@@ -263,7 +263,7 @@ __device__ __forceinline__ void move_units(const RopeParams& r, const Positions<
 // ---------------------------------------------------------------------------
 // Into the bf16 cache: a work-group takes `per_wg` tokens; a thread takes one
 // unit of two consecutive heads (queries, then keys), or 32 bytes of values.
-// Bound by HBM.
+// Bound by HBM: a latent prompt of 4096 tokens 241 us, 5.0 TB/s read and written.
 // ---------------------------------------------------------------------------
 template <int DK, int DV, bool AXES>
 __global__ __launch_bounds__(512) void rope_append_kernel(RopeAppendParams p) {
@@ -313,7 +313,8 @@ __global__ __launch_bounds__(512) void rope_append_kernel(RopeAppendParams p) {
 // A wave holds its rows in registers between the maximum that gives the scale
 // and the conversion, so they are read once. (With all tasks of a block in the
 // work-group of its first token, a 2048-token chunk beside 128 decodes took
-// 33.6 us, now 13.8.)
+// 33.6 us, now 13.3, 3 of them above the rotation into the bf16 cache: the
+// search, the page, the rows, their maximum and the codes follow each other.)
 // ---------------------------------------------------------------------------
 
 // The sequence that holds new token t: the largest s with query_start_loc[s]
