@@ -221,6 +221,26 @@ def test_strided_caches_and_rows():
     assert (scales[:, 0] == 0x55).all() and (scales[:, 2] == 0x55).all()
 
 
+def test_far_pages():
+    """Pages past 5 GiB of codes, with slots 80 KiB apart."""
+    c = Case(D64, *RAGGED, seed=12)
+    g = c.gpu()
+    used, gap = c.codes[0].shape[0], 80 << 10
+    far = (5 << 30) // (c.P * gap) + 1
+    pool = torch.zeros((far + used) * c.P * gap, dtype=torch.uint8, device="cuda")
+    wide = pool.as_strided((far + used, c.P, c.hkv, c.d), (c.P * gap, gap, c.d, 1))
+    wide[far:] = g["kc"].view(torch.uint8)
+    big = dict(g, kc=wide.view(torch.float8_e4m3fn), bt=g["bt"] + far)
+    for n in ("vc", "sc"):
+        x = torch.zeros((far + used, *g[n].shape[1:]), dtype=torch.uint8, device="cuda")
+        x[far:] = g[n].view(torch.uint8)
+        big[n] = x.view(g[n].dtype)
+    c.run(big)
+    torch.cuda.synchronize()
+    assert all(not big[n][:far].view(torch.uint8).any() for n in ("kc", "vc", "sc"))
+    c.check(dict(big, **{n: big[n][far:] for n in ("kc", "vc", "sc")}), "far")
+
+
 def test_twice_is_once_and_captured():
     """The same append again changes nothing, and replays of a captured one,
     with other work between, give what the eager call gives."""

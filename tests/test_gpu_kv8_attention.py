@@ -73,6 +73,19 @@ def test_decode(hq, hkv, d, P, opts):
     c.check(*c.run("decode", **opts), "decode")
 
 
+@pytest.mark.parametrize("hq,hkv,d,P", [(10, 5, 128, 16), (18, 9, 64, 64), (48, 6, 128, 64), (17, 17, 64, 16), (32, 8, 128, 16)])
+def test_decode_in_several_columns(hq, hkv, d, P):
+    """Rows of more than 512 bytes: work-groups of uneven groups of heads, pieces
+    and whole sequences, merged by columns and by rows."""
+    log(f"kv8 decode columns {hq}/{hkv} d{d} page {P}")
+    c = Case(hq, hkv, d, P, [1] * len(DECODES), DECODES, seed=hq + d)
+    assert c.plan().plan.info["decode_wg_width"] == -(-hkv * d // 512)
+    c.check(*c.run("decode"), "columns")
+    c.check(*c.run("decode", min_split_tokens=2048), "whole sequences")
+    c = Case(hq, hkv, d, P, [1, 1], [3000, 17], seed=hq)
+    c.check(*c.run("decode"), "many pieces")
+
+
 @pytest.mark.parametrize("hq,hkv,d,P", [(28, 4, 128, 16), (28, 4, 128, 64), (15, 5, 64, 16), (32, 8, 64, 64), (4, 1, 64, 16),
                                         (16, 1, 128, 64), (8, 8, 128, 16), (24, 12, 128, 64)])
 def test_prefill(hq, hkv, d, P):
