@@ -313,9 +313,6 @@ void prefill_kv8_kernel(AttnParams p) {
     }
   };
 
-  // Q must land before the loop: inside it vmcnt counts only the tile loads.
-  wait_vmem_all();
-
   // Past the barrier of step kt (every wave has written its part of the group's
   // tile and is done with the one before) the group's next tile is converted to
   // where the last one was, behind this one's scores, and the loads of the
@@ -332,7 +329,7 @@ void prefill_kv8_kernel(AttnParams p) {
     auto key_of = [&](int kt) { return wk0 + (kt * KG + group) * kKeys; };
     lds_barrier();
     for (int i = tid; i < pages; i += NT) pt[i] = bt_row[pt_base + i];
-    wait_vmem_all();
+    wait_vmem_all();   // Q too, the first time: in the loops vmcnt counts only the tile loads
     lds_barrier();
     if (ntiles > 0) loader.fetch(key_of(0), 0, loader.first_page(key_of(0), pt_base));
     if (ntiles > 1) loader.fetch(key_of(1), 1, loader.first_page(key_of(1), pt_base));
