@@ -142,9 +142,10 @@ struct Kv8AppendParams {
   int64_t scale_sp;
   int64_t num_pages;
   int32_t* bad_count;
+  int32_t waves;                        // of a token: 1, 2 or 4 (the launch sets it)
   RopeParams rope;
 };
 
-hipError_t launch_kv8_append(const Kv8AppendParams& p, int head_dim, hipStream_t stream);
+hipError_t launch_kv8_append(Kv8AppendParams p, int head_dim, hipStream_t stream);
 
 }  // namespace flexattn

@@ -306,10 +306,10 @@ __global__ __launch_bounds__(512) void rope_append_kernel(RopeAppendParams p) {
 }
 
 // ---------------------------------------------------------------------------
-// Into the 8-bit cache. Work-group t takes new token t: it finds the token's
-// sequence, turns its query, and takes its part of the token's block: a task is
-// the block's new rows of one KV head, K or V, for one wave, and the
-// work-groups of the block's new tokens (which are consecutive) share them out.
+// Into the 8-bit cache. One, two or four waves take a new token: they find the
+// token's sequence, turn its query, and take their part of the token's block: a
+// task is the block's new rows of one KV head, K or V, for one wave, and the
+// waves of the block's new tokens (which are consecutive) share them out.
 // A wave holds its rows in registers between the maximum that gives the scale
 // and the conversion, so they are read once. (With all tasks of a block in the
 // work-group of its first token, a 2048-token chunk beside 128 decodes took
@@ -462,11 +462,15 @@ struct Block {
   }
 };
 
+constexpr int kAppendWaves = 4;   // of a work-group
+
 template <int D, bool AXES>
-__global__ __launch_bounds__(256) void kv8_append_kernel(Kv8AppendParams p) {
+__global__ __launch_bounds__(64 * kAppendWaves) void kv8_append_kernel(Kv8AppendParams p) {
   constexpr int U = D / 16;
-  const int64_t t = blockIdx.x;
-  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int waves = p.waves, w = wave % waves;       // of the token
+  const int64_t t = int64_t(blockIdx.x) * (kAppendWaves / waves) + wave / waves;
+  if (t >= p.n_tokens) return;
   const bool rope = p.rope.cos_sin != nullptr;
   Positions<AXES> x;
   if (rope && p.rope.positions) x = read_positions<AXES>(p.rope, t);
@@ -481,7 +485,7 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(Kv8AppendParams p) {
   const bool in_row = pos >= 0 && page_at < p.bt_stride;
   const int32_t page = p.bt[int64_t(q.s) * p.bt_stride + (in_row ? page_at : 0)];
   if (rope) {
-    for (int u = threadIdx.x; u < (p.Hq + kHeadsPerThread - 1) / kHeadsPerThread * U; u += blockDim.x) {
+    for (int u = 64 * w + lane; u < (p.Hq + kHeadsPerThread - 1) / kHeadsPerThread * U; u += 64 * waves) {
       const int g = u / U;
       move_units(
           p.rope, x, u - g * U, g * kHeadsPerThread, p.Hq, [&] { return x.ok && in_row && page >= 0 && page < p.num_pages; },
@@ -489,9 +493,8 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(Kv8AppendParams p) {
     }
   }
   // The token's block holds `count` of the call's new rows, from row r0 on, and
-  // this token's is the `rank`-th: its work-group takes every count-th task (a
-  // KV head, or its K or V), from the last wave down (the first ones turn
-  // queries).
+  // this token's is the `rank`-th: its waves take every count-th task (a KV
+  // head, or its K or V), from the last wave down (the first ones turn queries).
   const int32_t first = max(pos & ~15, q.L - (q.end - max(q.start, 0)));   // position of the block's first new row
   const int r0 = first & 15, rank = pos - first;
   const int64_t tf = t - rank;
@@ -506,7 +509,7 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(Kv8AppendParams p) {
             kv ? p.v_ss : p.k_ss, p.scales + page * p.scale_sp + (row0 / 16 * p.Hkv + h) * 2 + kv, r0, lane);
   };
   const auto paged = [&] { return in_row && page >= 0 && page < p.num_pages; };
-  const int waves = blockDim.x / 64, mine = rank + (waves - 1 - w) * count;
+  const int mine = rank + (waves - 1 - w) * count;
   constexpr int RPP = 64 / U;
   if (count <= RPP) {          // one pass holds the rows: keys and values of a head side by side
     for (int h = mine; h < p.Hkv; h += waves * count) {
@@ -525,7 +528,7 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(Kv8AppendParams p) {
       write(b, task >> 1, task & 1);
     }
   }
-  if (threadIdx.x == 0 && !(x.ok && paged()) && p.bad_count) atomicAdd(p.bad_count, 1);
+  if (w == 0 && lane == 0 && !(x.ok && paged()) && p.bad_count) atomicAdd(p.bad_count, 1);
 }
 
 template <int DK, int DV, bool AXES>
@@ -566,14 +569,28 @@ hipError_t launch_rope_append(const RopeAppendParams& p, hipStream_t stream) {
   }
 }
 
-hipError_t launch_kv8_append(const Kv8AppendParams& p, int head_dim, hipStream_t stream) {
+hipError_t launch_kv8_append(Kv8AppendParams p, int head_dim, hipStream_t stream) {
   if (p.n_tokens == 0 || p.num_seqs == 0) return hipSuccess;
   if (p.n_tokens > INT32_MAX) return hipErrorInvalidValue;
   if (head_dim != 64 && head_dim != 128) return hipErrorInvalidValue;
   const bool axes = p.rope.n_axes > 1;
   const auto kern = head_dim == 128 ? (axes ? kv8_append_kernel<128, true> : kv8_append_kernel<128, false>)
                                     : (axes ? kv8_append_kernel<64, true> : kv8_append_kernel<64, false>);
-  hipLaunchKernelGGL(kern, dim3(uint32_t(p.n_tokens)), dim3(256), 0, stream, p);
+  // Waves of a token: four where calls are short, where a single token's tasks
+  // follow each other in fewer; fewer where tokens fill the machine many times
+  // over, most of all those of prompts, which share their block's tasks, with
+  // little to turn. One, two and four waves, us: 64 decode tokens of 28/4 heads
+  // of 128 12.3, 8.2, 6.0, 2048 of a prompt beside 128 19.2, 14.8, 13.8; prompts
+  // of 1 x 1024 9.3, 8.6, 7.5, 1 x 2048 11.7, 11.6, 11.5, 8 x 2048 65.5, 65.7,
+  // 68.9, on three axes 89.7, 103, 132; 8 x 2048 of 8/8 heads of 64 25.6, 28.4,
+  // 36.9, of 32/8 50.5, 48.0, 51.9, of 4/1 17.3, 22.4, 35.5; 4 x 2048 beside 128
+  // decodes, 28/4 of 128, 41.5, 39.2, 42.6.
+  const bool prompts = p.n_tokens >= int64_t(64) * p.num_seqs || p.Hkv == 1;   // or one task a token
+  const int units = (p.Hq + kHeadsPerThread - 1) / kHeadsPerThread * (head_dim / 16);
+  if (prompts && p.n_tokens >= 4096) p.waves = axes || units <= 32 ? 1 : 2;
+  else p.waves = p.n_tokens >= (prompts ? 2048 : 8192) ? 2 : 4;
+  const int64_t per = kAppendWaves / p.waves;
+  hipLaunchKernelGGL(kern, dim3(uint32_t((p.n_tokens + per - 1) / per)), dim3(64 * kAppendWaves), 0, stream, p);
   return hipGetLastError();
 }
 

@@ -103,6 +103,17 @@ def test_several_axes(sections, dealt):
     c.check(c.run(), f"axes {sections}")
 
 
+@pytest.mark.parametrize("geo,ns,axes", [
+    (QWEN, [2100], 1), (QWEN, [4099], 1), (D64, [1500, 1500, 1500], 3), (ONE, [1] * 500 + [1600], 1), (ONE, [1] * 500 + [3700], 3),
+    (ONE, [1] * 130 + [8200], 1)])
+def test_many_tokens(geo, ns, axes):
+    """Tokens by two waves and by one: prompts, and single tokens among them."""
+    log(f"kv8 append of {sum(ns)} tokens {geo} on {axes} axes")
+    kw = dict(sections=[8, 12, 12]) if axes > 1 else {}
+    c = Case(geo, ns, [n + 7 * i % 40 for i, n in enumerate(ns)], seed=len(ns), pad=5, max_pos=9000, **kw)
+    c.check(c.run(), "many tokens")
+
+
 def test_given_positions_are_the_tokens_own():
     a, b = Case(QWEN, *RAGGED, seed=6), Case(QWEN, *RAGGED, seed=6, positions=True)
     ga, gb = a.run(), b.run()
