@@ -142,7 +142,7 @@ struct Kv8AppendParams {
   int64_t scale_sp;
   int64_t num_pages;
   int32_t* bad_count;
-  int32_t waves;                        // of a token: 1, 2 or 4 (the launch sets it)
+  int32_t log_waves;                    // of a token: 0, 1 or 2 (the launch sets it)
   RopeParams rope;
 };
 

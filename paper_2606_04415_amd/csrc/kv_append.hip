@@ -261,9 +261,11 @@ __device__ __forceinline__ void move_units(const RopeParams& r, const Positions<
 }
 
 // ---------------------------------------------------------------------------
-// Into the bf16 cache: a work-group takes `per_wg` tokens; a thread takes one
-// unit of two consecutive heads (queries, then keys), or 32 bytes of values.
-// Bound by HBM: a latent prompt of 4096 tokens 241 us, 5.0 TB/s read and written.
+// Into the bf16 cache: a work-group takes `per_wg` tokens, or a part of one; a
+// thread takes one unit of two consecutive heads (queries, then keys), or 32
+// bytes of values. Bound by HBM: a latent prompt of 4096 tokens 241 us, 5.0 TB/s
+// read and written. (With the parts of a token in turn in one work-group, 16
+// latent tokens of 128 heads took 9.2 us, now 4.0, 256 16.3, now 15.6.)
 // ---------------------------------------------------------------------------
 template <int DK, int DV, bool AXES>
 __global__ __launch_bounds__(512) void rope_append_kernel(RopeAppendParams p) {
@@ -274,35 +276,35 @@ __global__ __launch_bounds__(512) void rope_append_kernel(RopeAppendParams p) {
   const int per_tok = nqk + nv, page_bits = __builtin_ctz(a.P);   // (pages of 16 or 64)
   const int64_t t0 = int64_t(blockIdx.x) * p.per_wg;
   const int n = int(min(int64_t(p.per_wg), a.n_tokens - t0)) * per_tok;
-  for (int i = threadIdx.x; i < n; i += blockDim.x) {
-    const int dt = p.per_wg == 1 ? 0 : i / per_tok;
-    const int u = i - dt * per_tok;
-    const int64_t t = t0 + dt;
-    const int32_t slot = a.slot_mapping[t];
-    const auto x = read_positions<AXES>(p.rope, t);
-    // A negative slot is padding; another fault is counted once a token.
-    const bool inside = slot >= 0 && int64_t(slot) < a.num_slots, live = inside && x.ok;
-    const int64_t page = inside ? slot >> page_bits : 0, row = inside ? slot & (a.P - 1) : 0;
-    if (u < nqk) {
-      const int g = u / UK;
-      move_units(
-          p.rope, x, u - g * UK, g * kHeadsPerThread, heads, [&] { return live; },
-          [&](int h) { return h < p.Hq ? p.q + t * p.q_stride + h * DK : a.k_new + t * a.k_new_stride + (h - p.Hq) * DK; },
-          [&](int h) {
-            return h < p.Hq ? p.q_out + (t * p.Hq + h) * DK
-                            : const_cast<uint16_t*>(a.kc.base) + page * a.kc.sp + row * a.kc.ss + (h - p.Hq) * a.kc.sh;
-          });
-    } else {
-      const int v = u - nqk, h = v / UV, c = 16 * (v - h * UV);
-      const uint16_t* src = a.v_new + t * a.v_new_stride + h * DV + c;
-      const u32x4 v0 = load16(src), v1 = load16(src + 8);
-      if (!live) continue;   // (never a token's unit 0)
-      uint16_t* dst = const_cast<uint16_t*>(a.vc.base) + page * a.vc.sp + row * a.vc.ss + h * a.vc.sh + c;
-      *reinterpret_cast<u32x4*>(dst) = v0;
-      *reinterpret_cast<u32x4*>(dst + 8) = v1;
-    }
-    if (u == 0 && slot >= 0 && !live && a.bad_count) atomicAdd(a.bad_count, 1);
+  const int i = blockIdx.y * blockDim.x + threadIdx.x;
+  if (i >= n) return;
+  const int dt = p.per_wg == 1 ? 0 : i / per_tok;
+  const int u = i - dt * per_tok;
+  const int64_t t = t0 + dt;
+  const int32_t slot = a.slot_mapping[t];
+  const auto x = read_positions<AXES>(p.rope, t);
+  // A negative slot is padding; another fault is counted once a token.
+  const bool inside = slot >= 0 && int64_t(slot) < a.num_slots, live = inside && x.ok;
+  const int64_t page = inside ? slot >> page_bits : 0, row = inside ? slot & (a.P - 1) : 0;
+  if (u < nqk) {
+    const int g = u / UK;
+    move_units(
+        p.rope, x, u - g * UK, g * kHeadsPerThread, heads, [&] { return live; },
+        [&](int h) { return h < p.Hq ? p.q + t * p.q_stride + h * DK : a.k_new + t * a.k_new_stride + (h - p.Hq) * DK; },
+        [&](int h) {
+          return h < p.Hq ? p.q_out + (t * p.Hq + h) * DK
+                          : const_cast<uint16_t*>(a.kc.base) + page * a.kc.sp + row * a.kc.ss + (h - p.Hq) * a.kc.sh;
+        });
+  } else {
+    const int v = u - nqk, h = v / UV, c = 16 * (v - h * UV);
+    const uint16_t* src = a.v_new + t * a.v_new_stride + h * DV + c;
+    const u32x4 v0 = load16(src), v1 = load16(src + 8);
+    if (!live) return;   // (never a token's unit 0)
+    uint16_t* dst = const_cast<uint16_t*>(a.vc.base) + page * a.vc.sp + row * a.vc.ss + h * a.vc.sh + c;
+    *reinterpret_cast<u32x4*>(dst) = v0;
+    *reinterpret_cast<u32x4*>(dst + 8) = v1;
   }
+  if (u == 0 && slot >= 0 && !live && a.bad_count) atomicAdd(a.bad_count, 1);
 }
 
 // ---------------------------------------------------------------------------
@@ -468,8 +470,8 @@ template <int D, bool AXES>
 __global__ __launch_bounds__(64 * kAppendWaves) void kv8_append_kernel(Kv8AppendParams p) {
   constexpr int U = D / 16;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int waves = p.waves, w = wave % waves;       // of the token
-  const int64_t t = int64_t(blockIdx.x) * (kAppendWaves / waves) + wave / waves;
+  const int waves = 1 << p.log_waves, w = wave & (waves - 1);   // of the token
+  const int64_t t = (int64_t(blockIdx.x) * kAppendWaves + wave) >> p.log_waves;
   if (t >= p.n_tokens) return;
   const bool rope = p.rope.cos_sin != nullptr;
   Positions<AXES> x;
@@ -533,16 +535,15 @@ __global__ __launch_bounds__(64 * kAppendWaves) void kv8_append_kernel(Kv8Append
 
 template <int DK, int DV, bool AXES>
 hipError_t launch_rope_append_t(RopeAppendParams p, hipStream_t stream) {
-  // Work-groups of up to 512 threads: a token's units, or those of as many
-  // tokens as 512 threads cover at one unit each; when a token has more, as
-  // few threads as take them in the same number of rounds.
+  // Work-groups of up to 512 threads, a unit each: those of as many tokens as
+  // 512 threads cover, or of one, in as few equal parts as take them.
   const int units = (p.Hq + p.Hkv + kHeadsPerThread - 1) / kHeadsPerThread * (DK / 16) + (p.kv.cv ? p.Hkv * (DV / 16) : 0);
   p.per_wg = int32_t(std::min<int64_t>(std::max(1, 512 / units), p.kv.n_tokens));
-  const int n = units * p.per_wg, rounds = (n + 511) / 512;
-  const int threads = ((n + rounds - 1) / rounds + 63) / 64 * 64;
+  const int n = units * p.per_wg, parts = (n + 511) / 512;
+  const int threads = ((n + parts - 1) / parts + 63) / 64 * 64;
   const int64_t blocks = (p.kv.n_tokens + p.per_wg - 1) / p.per_wg;
   if (blocks > INT32_MAX) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((rope_append_kernel<DK, DV, AXES>), dim3(uint32_t(blocks)), dim3(threads), 0, stream, p);
+  hipLaunchKernelGGL((rope_append_kernel<DK, DV, AXES>), dim3(uint32_t(blocks), parts), dim3(threads), 0, stream, p);
   return hipGetLastError();
 }
 
@@ -587,10 +588,10 @@ hipError_t launch_kv8_append(Kv8AppendParams p, int head_dim, hipStream_t stream
   // decodes, 28/4 of 128, 41.5, 39.2, 42.6.
   const bool prompts = p.n_tokens >= int64_t(64) * p.num_seqs || p.Hkv == 1;   // or one task a token
   const int units = (p.Hq + kHeadsPerThread - 1) / kHeadsPerThread * (head_dim / 16);
-  if (prompts && p.n_tokens >= 4096) p.waves = axes || units <= 32 ? 1 : 2;
-  else p.waves = p.n_tokens >= (prompts ? 2048 : 8192) ? 2 : 4;
-  const int64_t per = kAppendWaves / p.waves;
-  hipLaunchKernelGGL(kern, dim3(uint32_t((p.n_tokens + per - 1) / per)), dim3(64 * kAppendWaves), 0, stream, p);
+  if (prompts && p.n_tokens >= 4096) p.log_waves = axes || units <= 32 ? 0 : 1;
+  else p.log_waves = p.n_tokens >= (prompts ? 2048 : 8192) ? 1 : 2;
+  const int64_t blocks = ((p.n_tokens << p.log_waves) + kAppendWaves - 1) / kAppendWaves;
+  hipLaunchKernelGGL(kern, dim3(uint32_t(blocks)), dim3(64 * kAppendWaves), 0, stream, p);
   return hipGetLastError();
 }
 
