@@ -98,7 +98,8 @@ typedef struct flex_attn_plan_opts {
                                  such 128-row work-groups, or, on a co-run share, when all of
                                  them fit in one round (three per CU); else 32]; 576/512: 64
                                  or 128 tokens [128]; 192/128: 128 [128] */
-  int32_t min_split_tokens;   /* shortest balanced decode range, in keys [256; 64 with kv_bits 8] */
+  int32_t min_split_tokens;   /* shortest balanced decode range, in keys [256; with kv_bits 8 64, or
+                                 what the decode sequences have in the mean if that is less] */
   int32_t wg_per_cu;          /* decode work-groups aimed at per CU
                                  [1 grouped-query, 2 for 576/512] */
   int32_t split_granule;      /* co-run split granularity in CUs [32] */

@@ -23,7 +23,12 @@ the contract is:
   128 divides Hq, else Hq / 64). The list is cut into
   R = max(1, min(floor(cus_decode * wg_per_cu / W), floor(T / min_pps)),
   ceil(T / 8192)) ranges, range r = pages [floor(r T / R), floor((r + 1) T / R)),
-  min_pps = ceil(min_split_tokens / P). A piece is the non-empty overlap of a
+  min_pps = ceil(min_split_tokens / P), by default for 8-bit caches no more than
+  ceil(T / decode sequences). (By default for 8-bit caches, where no decode
+  sequence is longer than 256 keys, 128 for fewer than 16 of them, and there is
+  no tail, ranges hold whole sequences: R = max(1, min(floor(cus_decode *
+  wg_per_cu / W), their number n)), range r = sequences [floor(r n / R),
+  floor((r + 1) n / R)).) A piece is the non-empty overlap of a
   range with one sequence, keys [k0, k1) = [first page * P,
   min(L_s, end page * P)); pieces are listed by range, i.e. in batch order
   with keys ascending, and the list index is the piece's workspace slot.
@@ -300,6 +305,8 @@ def build_plan(sh: Shape, opts: Optional[Opts], qsl: Sequence[int], seq_lens: Se
     # cost model: what the decode share covers during the prefill plus its share
     # of the rest at the device's streaming rate
     min_pps = cdiv(min_tokens, P)
+    if o.kv_bits == 8 and not o.min_split_tokens and dec:
+        min_pps = min(min_pps, max(1, cdiv(sum(cdiv(seq_lens[s], P) for s in dec), len(dec))))
     pages = [cdiv(seq_lens[s], P) for s in dec]
     T = sum(pages)
     TA = T
@@ -322,7 +329,11 @@ def build_plan(sh: Shape, opts: Optional[Opts], qsl: Sequence[int], seq_lens: Se
         if npages == 0:
             return 0
         return max(1, min((cus * wg_per_cu) // W, npages // min_pps), cdiv(npages, MAX_RANGE_PAGES))
-    RA = n_ranges(TA, cus_decode) if dec else 0
+    longest = max([seq_lens[s] for s in dec], default=0)
+    whole_ranges = max(1, min((cus_decode * wg_per_cu) // W, len(dec)))
+    whole = (o.kv_bits == 8 and not o.min_split_tokens and dec and TB == 0 and longest <= (128 if len(dec) < 16 else 256)
+             and cdiv(len(dec), whole_ranges) * cdiv(longest, P) <= MAX_RANGE_PAGES)
+    RA = 0 if not dec else whole_ranges if whole else n_ranges(TA, cus_decode)
     RB = n_ranges(TB, cus_prefill) if dec else 0
     R = RA + RB
     bounds = ([(r * TA) // RA for r in range(RA + 1)] + [TA + (r * TB) // RB for r in range(1, RB + 1)]
@@ -330,6 +341,8 @@ def build_plan(sh: Shape, opts: Optional[Opts], qsl: Sequence[int], seq_lens: Se
     start = [0]
     for n_p in pages:
         start.append(start[-1] + n_p)       # first global page of each decode sequence
+    if whole:
+        bounds = [start[r * len(dec) // RA] for r in range(RA + 1)]
     pieces, ranges = [], []
     for r in range(R):
         ranges.append(len(pieces))
@@ -349,6 +362,8 @@ def build_plan(sh: Shape, opts: Optional[Opts], qsl: Sequence[int], seq_lens: Se
             dec_items.append((i, [s, j, len(mine), pieces[i][2], pieces[i][3], mine[0], qsl[s], i]))
     dec_items = [it for _, it in sorted(dec_items, key=lambda x: x[0])]
     ppr = max(cdiv(TA, RA) if RA else 0, cdiv(TB, RB) if RB else 0)
+    if whole:
+        ppr = max([ppr] + [b - a for a, b in zip(bounds, bounds[1:])])
 
     # --- prefill tiles, longest key range first
     tiles = []

@@ -300,10 +300,15 @@ extern "C" int flex_attn_plan(const flex_attn_shape* shape, const flex_attn_plan
   // once the prefill is done (both groups then stream together until both
   // end). TA follows the cost model: what the decode share covers during the
   // prefill, plus its share of the rest at the device's streaming rate.
-  const int64_t min_pps = cdiv(min_tokens, P);
   std::vector<int64_t> start(dec.size() + 1, 0);   // first global page of each decode sequence
   for (size_t d = 0; d < dec.size(); ++d) start[d + 1] = start[d] + cdiv(seq_lens[dec[d]], P);
   const int64_t T = start[dec.size()];
+  // (Over an 8-bit cache, unless the caller sets it, no more than the
+  // sequences have in the mean: a work-group takes its range's sequences one
+  // after the other. 28/4 heads of 128, us: 9 sequences of 2 keys 19.5 in 2
+  // ranges, 6.6 in 9; 160 of 2 to 9 16.4 in 40, 6.8 in 160.)
+  int64_t min_pps = cdiv(min_tokens, P);
+  if (kv8 && o.min_split_tokens == 0 && !dec.empty()) min_pps = std::min(min_pps, std::max<int64_t>(1, cdiv(T, int64_t(dec.size()))));
   int64_t TA = T;
   if (!latent && !split && o.decode_tail == 0 && cus_prefill < cus_total && T > 1) {
     const double hbm = (o.hbm_gbps != 0.0 ? o.hbm_gbps : kDefaultHbmGBps) * 1e9;
@@ -328,10 +333,21 @@ extern "C" int flex_attn_plan(const flex_attn_shape* shape, const flex_attn_plan
     return std::max<int64_t>({int64_t(1), std::min<int64_t>(cus * wg_per_cu / W, pages / min_pps),
                               cdiv(pages, kMaxRangePages)});
   };
-  const int64_t RA = dec.empty() ? 0 : n_ranges(TA, cus_decode);
+  // Over an 8-bit cache, where all sequences are short and there is no tail:
+  // ranges of whole sequences, which need no merge. By pages and whole, 28/4
+  // heads of 128, us: 64 of 10 to 60 keys 15.2 and 6.7, 20 of 5 to 200 15.1 and
+  // 11.8, 256 of 100 to 256 22.3 and 13.3, 8 of these 12.0 and 11.8; but one of
+  // 256 8.3 and 11.3, 16 of 50 to 500 13.1 and 19.1.
+  const int64_t nd = int64_t(dec.size()), whole_ranges = std::max<int64_t>(1, std::min<int64_t>(cus_decode * wg_per_cu / W, nd));
+  int64_t longest_dec = 0;
+  for (int32_t s : dec) longest_dec = std::max<int64_t>(longest_dec, seq_lens[s]);
+  const bool whole = kv8 && o.min_split_tokens == 0 && nd > 0 && TB == 0 && longest_dec <= (nd < 16 ? 128 : 256) &&
+                     cdiv(nd, whole_ranges) * cdiv(longest_dec, P) <= kMaxRangePages;
+  const int64_t RA = dec.empty() ? 0 : whole ? whole_ranges : n_ranges(TA, cus_decode);
   const int64_t RB = dec.empty() ? 0 : n_ranges(TB, cus_prefill);
   const int64_t R = RA + RB;
   auto bound = [&](int64_t r) -> int64_t {   // first page of range r
+    if (whole) return start[r * nd / R];
     return r <= RA ? r * TA / std::max<int64_t>(RA, 1) : TA + (r - RA) * TB / RB;
   };
   struct Piece { int32_t s, d, k0, k1; };
@@ -351,7 +367,8 @@ extern "C" int flex_attn_plan(const flex_attn_shape* shape, const flex_attn_plan
     }
   }
   ranges.push_back(int32_t(pieces.size()));
-  const int64_t ppr = std::max(RA ? cdiv(TA, RA) : 0, RB ? cdiv(TB, RB) : 0);   // most pages of a range
+  int64_t ppr = std::max(RA ? cdiv(TA, RA) : 0, RB ? cdiv(TB, RB) : 0);   // most pages of a range
+  for (int64_t r = 0; whole && r < R; ++r) ppr = std::max(ppr, bound(r + 1) - bound(r));
   std::vector<int32_t> first_piece(dec.size(), -1), n_pieces(dec.size(), 0);
   for (size_t i = 0; i < pieces.size(); ++i) {
     const int32_t d = pieces[i].d;

@@ -73,6 +73,16 @@ def test_decode(hq, hkv, d, P, opts):
     c.check(*c.run("decode", **opts), "decode")
 
 
+@pytest.mark.parametrize("hq,hkv,d,P", [(28, 4, 128, 16), (32, 8, 64, 64), (32, 8, 128, 16), (4, 1, 64, 16)])
+@pytest.mark.parametrize("count,top", [(1, 1), (3, 128), (40, 256), (600, 20)])
+def test_decode_of_short_sequences(hq, hkv, d, P, count, top):
+    """Ranges of whole sequences: one each, or several of every length after each other."""
+    log(f"kv8 decode {hq}/{hkv} d{d} page {P}: {count} of up to {top}")
+    c = Case(hq, hkv, d, P, [1] * count, [top] + [1 + (37 * i) % top for i in range(count - 1)], seed=count)
+    assert c.plan().plan.info["n_split_seqs"] == 0
+    c.check(*c.run("decode"), "short")
+
+
 @pytest.mark.parametrize("hq,hkv,d,P", [(10, 5, 128, 16), (18, 9, 64, 64), (48, 6, 128, 64), (17, 17, 64, 16), (32, 8, 128, 16)])
 def test_decode_in_several_columns(hq, hkv, d, P):
     """Rows of more than 512 bytes: work-groups of uneven groups of heads, pieces

@@ -113,6 +113,28 @@ def test_plans_for_8_bit_caches_match_the_rederivation():
                             bm=rng.choice([0, 128]), decode_tail=rng.choice([0, -1])), qsl, ls, maxp)
 
 
+@pytest.mark.parametrize("count,top,whole", [(1, 128, True), (1, 129, False), (9, 2, True), (15, 129, False), (16, 256, True), (16, 257, False),
+                                             (700, 250, True), (3000, 5, True), (300, 3000, False)])
+@pytest.mark.parametrize("co", [0, 96])
+def test_short_decode_sequences_stay_whole(count, top, whole, co):
+    """Ranges of whole sequences by default, beside a prefill too; by pages when
+    the caller sets the least range; no range shorter than the mean sequence."""
+    rng = random.Random(count * top)
+    ls = [top] + [rng.randint(1, top) for _ in range(count - 1)]
+    ns = [1] * count + ([40] if co else [])
+    ls += [40] if co else []
+    qsl = np.concatenate([[0], np.cumsum(ns)]).astype(int).tolist()
+    for sh in GQA:
+        maxp = max(-(-x // sh.page_size) for x in ls)
+        shape = F.make_shape(sh.num_q_heads, sh.num_kv_heads, sh.head_dim_qk, sh.head_dim_v, sh.page_size, sh.sm_scale)
+        for kw in ({}, dict(min_split_tokens=64)):
+            compare(sh, OP.Opts(kv_bits=8, cus_decode=co, decode_tail=-1 if co else 0, **kw), qsl, ls, maxp)
+        i = F.flex_attn_plan(shape, F.make_opts(kv_bits=8, cus_decode=co, decode_tail=-1 if co else 0), qsl, ls, maxp).info
+        assert (i["n_split_seqs"] == 0 and i["n_decode_items"] == count) or not whole
+        assert not whole or i["n_decode_ranges"] == min(count, (co or 256) // i["decode_wg_width"])
+        assert i["n_decode_ranges"] <= max(count, sum(-(-x // sh.page_size) for x in ls[:count]) * sh.page_size // 64)
+
+
 @pytest.mark.parametrize("n,ls,cut", [((64,), (4000,), True), ((2,), (300,), False), ((2,), (448,), False), ((2,), (449,), True), ((64, 3), (64, 2500), True),
                                       ((64, 1, 200), (4000, 900, 210), True), ((3000,), (3000,), False), ((200,) * 5, (3000,) * 5, False)])
 def test_few_prefill_tiles_are_cut_along_their_keys(n, ls, cut):
