@@ -130,8 +130,8 @@ typedef struct flex_attn_plan_info {
   int32_t n_decode_seqs;     /* sequences with one new token (none in the 192/128 layout) */
   int32_t n_prefill_seqs;    /* sequences with two or more new tokens (one or more: 192/128) */
   int32_t n_decode_items;    /* decode pieces: (sequence, key range) work items */
-  int32_t n_prefill_items;   /* (sequence, row tile) work items; with kv_bits 8 a tile of a few
-                                on a long prefix may be cut along its keys into several */
+  int32_t n_prefill_items;   /* (sequence, row tile) work items; with kv_bits 8 tiles that do not
+                                fill the device may be cut along their keys into several */
   int32_t n_split_seqs;      /* decode sequences cut into more than one piece */
   int32_t decode_wg_width;   /* work-groups per decode range or piece (grid y) */
   int32_t n_decode_ranges;   /* balanced page ranges the decode pieces form */

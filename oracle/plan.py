@@ -54,9 +54,11 @@ the contract is:
   Plans for 8-bit caches (kv_bits 8, grouped-query heads only) always take 128;
   their decode bytes count one byte a value and two scale bytes for each 16
   tokens and KV head, and a decode work-group covers ceil(Hkv / C) KV heads, C =
-  ceil(Hkv * d / 512). With N tiles of U_i = ceil(key_end / 64) units, for at
-  most half of the CUs (2 N * Hkv <= cus_prefill), and p >= 2 the least for
-  which Hkv * sum ceil(U_i / p) <= cus_prefill: if (max U_i - p) * 64 >= 384, a
+  ceil(Hkv * d / 512). With N tiles of U_i = ceil(key_end / 64) units and p(S)
+  >= 2 the least piece for which Hkv * sum ceil(U_i / p) <= S: for at most half
+  of the CUs (2 N * Hkv <= cus_prefill), p = p(cus_prefill) if (max U_i - p) *
+  64 >= 384; for N * Hkv <= 2 cus_prefill else, p = p(3 cus_prefill) if a model
+  of rates says that the longest tile alone lasts longer (cut_tiles). Then a
   tile is cut into n_i = ceil(U_i / p) pieces, the j-th over units
   [floor(j U_i / n_i), floor((j + 1) U_i / n_i)); item words 5 to 7 hold its first key and, where
   n_i > 1, n_i and its workspace slot (counted in tile order). Items are then
@@ -378,7 +380,7 @@ def build_plan(sh: Shape, opts: Optional[Opts], qsl: Sequence[int], seq_lens: Se
             tiles.append([s, t, r0, r1, L - n + last_token + 1, 0, 0, 0])
     n_pre_pieces = 0
     if o.kv_bits == 8:
-        tiles, n_pre_pieces = cut_tiles(tiles, sh.num_kv_heads, cus_prefill)
+        tiles, n_pre_pieces = cut_tiles(tiles, sh.num_kv_heads, cus_prefill, sh.head_dim_qk)
     tiles.sort(key=lambda it: (it[5] - it[4], it[0], it[1], it[5]))
 
     nd_, np_ = len(dec_items), len(tiles)
@@ -422,16 +424,35 @@ def build_plan(sh: Shape, opts: Optional[Opts], qsl: Sequence[int], seq_lens: Se
     return PlanResult(OK, blob, info)
 
 
-def cut_tiles(tiles, kv_heads: int, cus: int):
-    """Prefill tiles of a plan for an 8-bit cache, those that would leave compute
-    units idle cut along their keys (see the module contract); and the pieces."""
+def cut_tiles(tiles, kv_heads: int, cus: int, d: int):
+    """Prefill tiles of a plan for an 8-bit cache, cut along their keys where
+    that shortens the whole (see the module contract); and the pieces."""
     units = [cdiv(t[4], 64) for t in tiles]
-    if not tiles or 2 * len(tiles) * kv_heads > cus:
+    wgs = len(tiles) * kv_heads
+    if not tiles or wgs > 2 * cus:
         return tiles, 0
-    piece = 2
-    while sum(cdiv(u, piece) for u in units) * kv_heads > cus:
-        piece += 1
-    if (max(units) - piece) * 64 < 384:
+    longest, total = max(units), sum(units)
+
+    def shortest_piece(slots):
+        piece = 2
+        while sum(cdiv(u, piece) for u in units) * kv_heads > slots:
+            piece += 1
+        return piece
+    piece = longest
+    if 2 * wgs <= cus:
+        p1 = shortest_piece(cus)
+        if (longest - p1) * 64 >= 384:
+            piece = p1
+    else:
+        alone, beside, full, merge = (78.0, 54.0, 90.0, 16.0) if d == 64 else (49.0, 32.0, 57.0, 24.0)
+        at_once = (2 if d == 64 else 1) * cus
+        keys = sorted((t[4] for t in tiles), reverse=True)
+        few = wgs <= cus or (wgs > at_once and at_once // cus * keys[0] >= 768 and at_once // cus * (
+            keys[(at_once - 1) // kv_heads] + keys[at_once // kv_heads]) <= keys[0])   # two key groups, alone on their unit
+        whole = float(longest * 64) / (alone if few else beside)
+        if float(total * 64 * kv_heads) / (float(cus) * full) + merge < whole:
+            piece = shortest_piece(3 * cus)
+    if piece >= longest:
         return tiles, 0
     out, slot = [], 0
     for t, u in zip(tiles, units):

@@ -108,6 +108,19 @@ constexpr int kKv8Block = 16;
 // 16.4. Where 320 keys and 256 are gained: 4 prompts of 128 on 500 22.0 and
 // 25.8, one of 512 19.6 and 20.9.
 constexpr int64_t kKv8PieceKeys = 64, kKv8MinPiece = 128, kKv8PieceGain = 384;
+// Rates of prefill over an 8-bit cache, keys a us: of a work-group that has its
+// compute unit alone (two key groups) or shares it with another, and of a unit
+// whose resident work-groups are all there; us that the merge of so many pieces
+// adds. Measured; whole tiles and cut ones by the rule that uses them, 28/4
+// heads of 128, us: 7 prompts of 170 on 6000 keys 205 and 146, one of 1200 on
+// 4000 164 and 111, of 1024 on 4000 109 and 95, 3 of 512 on 2000 93 and 81; not
+// cut by it: 8 of 200 on 500 33 and 40, 2 of 1024 on 1000 70 and 74, one of 2048
+// 56 and 58. 32/8 of 64: 1200 on 4000 96 and 78; not 2048 on 4096, 124 and 126,
+// nor 2048, 39 and 42.
+struct Kv8CutModel {
+  double alone, beside, full, merge;
+};
+constexpr Kv8CutModel kKv8Cut128{49.0, 32.0, 57.0, 24.0}, kKv8Cut64{78.0, 54.0, 90.0, 16.0};
 
 // Rows (query heads) one decode work-group owns in the 576/512 layout.
 constexpr int kLatentRowsPerWG = 64;       // latent heads must be a multiple of this

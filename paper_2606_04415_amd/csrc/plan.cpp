@@ -13,6 +13,7 @@
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
+#include <functional>
 #include <new>
 #include <string>
 
@@ -401,27 +402,65 @@ extern "C" int flex_attn_plan(const flex_attn_shape* shape, const flex_attn_plan
       tiles.push_back({s, t, r0, r1, L - n + (flat ? (r1 - 1) / G + 1 : r1), 0, 0, 0});
     }
   }
-  // Over an 8-bit cache, tiles that would leave half of the compute units idle
-  // are cut along their keys too (pieces of whole kKv8PieceKeys, joined by a
-  // merge that follows the prefill): into the shortest pieces of at least
-  // kKv8MinPiece keys that have a compute unit each, when that shortens the
-  // longest tile by kKv8PieceGain keys or more. (The first piece of a tile has
-  // key_begin 0.)
+  // Two key groups a work-group over an 8-bit cache where all of them run at
+  // once (a compute unit holds one of heads of 128, two of 64) and have enough
+  // keys to share, or where those that wait, which are the shortest, end no
+  // later than the longest. One group and two, 28/4 heads of 128, us: a prompt
+  // of 512 21.7 and 19.4, of 1024 on 4000 keys 143 and 110, of 2048 (448
+  // work-groups) 67.9 and 57.2, two of 1024 40.7 and 37.6; but one of 64 8.1 and
+  // 9.3, 8 of 256 17.5 and 22.9, 4 of 512 25.7 and 27.8, one of 2500 82.0 and
+  // 84.1, of 1200 on 4000 165 and 182. 32/8 heads of 64: 1024 on 4000 100 and
+  // 71, 2048 on 4096 136 and 124, 2500 56.3 and 48.3; 8 of 256 12.4 and 13.3, 2
+  // of 1500 39.4 and 42.3.
+  const int64_t resident = sh.head_dim_qk == 64 ? 2 : 1, at_once = resident * cus_prefill;
+  auto two_key_groups = [&] {
+    if (tiles.empty()) return false;
+    std::vector<int64_t> keys;
+    for (const Tile& t : tiles) keys.push_back(t.kend - t.kbeg);
+    std::sort(keys.begin(), keys.end(), std::greater<int64_t>());
+    const int64_t wgs = int64_t(tiles.size()) * sh.num_kv_heads;
+    auto of = [&](int64_t wg) { return keys[size_t(wg / sh.num_kv_heads)]; };   // of a work-group, the longest first
+    if (wgs <= at_once) return keys[0] >= (wgs <= cus_prefill ? 256 : 512);
+    return resident * keys[0] >= 768 && resident * (of(at_once - 1) + of(at_once)) <= keys[0];
+  };
+  // Over an 8-bit cache, prefill tiles may be cut along their keys (into pieces
+  // of whole kKv8PieceKeys, joined by a merge that follows the prefill; the
+  // first piece of a tile has key_begin 0). Where they would leave half of the
+  // compute units idle: into the shortest pieces of at least kKv8MinPiece keys
+  // that have a compute unit each, when that shortens the longest tile by
+  // kKv8PieceGain keys or more. Where they are up to two a unit and the longest
+  // lasts longer than all of them would, spread evenly: into pieces that fill
+  // the resident work-groups (Kv8CutModel).
   int32_t n_pre_pieces = 0;   // of cut tiles
-  if (kv8 && !tiles.empty() && 2 * int64_t(tiles.size()) * sh.num_kv_heads <= cus_prefill) {
+  const int64_t whole_wgs = int64_t(tiles.size()) * sh.num_kv_heads;
+  if (kv8 && !tiles.empty() && whole_wgs <= 2 * cus_prefill) {
     int64_t longest = 0, total = 0;   // in units of kKv8PieceKeys
     for (const Tile& t : tiles) {
       longest = std::max(longest, cdiv(t.kend, kKv8PieceKeys));
       total += cdiv(t.kend, kKv8PieceKeys);
     }
-    int64_t piece = std::max(kKv8MinPiece / kKv8PieceKeys, cdiv(total * sh.num_kv_heads, cus_prefill));
-    auto work_groups = [&] {
-      int64_t n = 0;
-      for (const Tile& t : tiles) n += cdiv(cdiv(t.kend, kKv8PieceKeys), piece);
-      return n * sh.num_kv_heads;
+    auto shortest_piece = [&](int64_t slots) {   // with which pieces and heads make at most `slots` work-groups
+      int64_t piece = std::max(kKv8MinPiece / kKv8PieceKeys, cdiv(total * sh.num_kv_heads, slots));
+      auto work_groups = [&] {
+        int64_t n = 0;
+        for (const Tile& t : tiles) n += cdiv(cdiv(t.kend, kKv8PieceKeys), piece);
+        return n * sh.num_kv_heads;
+      };
+      while (work_groups() > slots) ++piece;
+      return piece;
     };
-    while (work_groups() > cus_prefill) ++piece;
-    if ((longest - piece) * kKv8PieceKeys >= kKv8PieceGain) {
+    int64_t piece = longest;
+    if (2 * whole_wgs <= cus_prefill) {
+      const int64_t p1 = shortest_piece(cus_prefill);
+      if ((longest - p1) * kKv8PieceKeys >= kKv8PieceGain) piece = p1;
+    } else {
+      const Kv8CutModel& m = sh.head_dim_qk == 64 ? kKv8Cut64 : kKv8Cut128;
+      const bool alone = whole_wgs <= cus_prefill || (whole_wgs > at_once && two_key_groups());
+      const double whole = double(longest * kKv8PieceKeys) / (alone ? m.alone : m.beside);
+      const double spread = double(total * kKv8PieceKeys * sh.num_kv_heads) / (double(cus_prefill) * m.full) + m.merge;
+      if (spread < whole) piece = shortest_piece(kFlatResidentPerCu * cus_prefill);
+    }
+    if (piece < longest) {
       std::vector<Tile> cut;
       for (const Tile& t : tiles) {
         const int64_t units = cdiv(t.kend, kKv8PieceKeys), pieces = cdiv(units, piece);
@@ -596,28 +635,7 @@ extern "C" int flex_attn_plan(const flex_attn_shape* shape, const flex_attn_plan
   // Behind it, per (piece of a cut prefill tile, KV head) the same of its 128 rows.
   plan->pre_ws_offset = size_t(cdiv(int64_t(ws), 256) * 256);
   plan->n_pre_pieces = n_pre_pieces;
-  // Two key groups a work-group where all of them run at once (a compute unit
-  // holds one of heads of 128, two of 64) and have enough keys to share, or
-  // where those that wait, which are the shortest, end no later than the
-  // longest. One group and two, 28/4 heads of 128, us: a prompt of 512 21.7 and
-  // 19.4, of 1024 on 4000 keys 143 and 110, of 2048 (448 work-groups) 67.9 and
-  // 57.2, two of 1024 40.7 and 37.6; but one of 64 8.1 and 9.3, 8 of 256 17.5
-  // and 22.9, 4 of 512 25.7 and 27.8, one of 2500 82.0 and 84.1, of 1200 on
-  // 4000 165 and 182. 32/8 heads of 64: 1024 on 4000 100 and 71, 2048 on 4096
-  // 136 and 124, 2500 56.3 and 48.3; 8 of 256 12.4 and 13.3, 2 of 1500 39.4 and
-  // 42.3.
-  plan->key_groups = 1;
-  if (kv8 && !tiles.empty()) {
-    const int64_t resident = sh.head_dim_qk == 64 ? 2 : 1;
-    const int64_t wgs = int64_t(tiles.size()) * sh.num_kv_heads, at_once = resident * cus_prefill;
-    auto keys = [&](int64_t wg) -> int64_t {   // of a work-group, the longest first
-      const Tile& t = tiles[wg / sh.num_kv_heads];
-      return t.kend - t.kbeg;
-    };
-    if (wgs <= at_once ? keys(0) >= (wgs <= cus_prefill ? 256 : 512)
-                       : resident * keys(0) >= 768 && resident * (keys(at_once - 1) + keys(at_once)) <= keys(0))
-      plan->key_groups = 2;
-  }
+  plan->key_groups = kv8 && two_key_groups() ? 2 : 1;
   if (n_pre_pieces > 0) ws = plan->pre_ws_offset + size_t(n_pre_pieces) * sh.num_kv_heads * 128 * (2 + sh.head_dim_v) * 4;
   flex_attn_plan_info& info = plan->info;
   std::memset(&info, 0, sizeof(info));

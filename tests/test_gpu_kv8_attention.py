@@ -232,6 +232,19 @@ def test_prefill_tiles_cut_along_their_keys(hq, hkv, d, P, ns, ls):
     c.check(out[0], None, "cut tiles, no log-sum-exp")
 
 
+@pytest.mark.parametrize("hq,hkv,d,P,ns,ls,cut", [
+    (28, 4, 128, 16, [85, 300, 85, 300, 85, 310], [2500, 3700, 2510, 3600, 85, 3711], False),
+    (28, 4, 128, 16, [100] * 12, [3011 + 40 * k for k in range(12)], True), (32, 8, 64, 64, [300] * 4, [3100, 3001, 2999, 3200], True)])
+def test_many_prefill_tiles_cut_along_their_keys(hq, hkv, d, P, ns, ls, cut):
+    """More tiles than compute units, long ones: spread over all that is
+    resident, but not where a few short ones are over."""
+    c = Case(hq, hkv, d, P, ns, ls, seed=21)
+    i, whole = c.plan().plan.info, sum(-(-n * (hq // hkv) // 128) for n in ns)
+    assert whole * hkv > i["cus_prefill"] and (i["n_prefill_items"] > 1.5 * whole) == cut
+    assert i["n_prefill_items"] * hkv <= 3 * i["cus_prefill"]
+    c.check(*c.run(), "spread")
+
+
 def test_cut_prefill_tiles_captured():
     c = Case(28, 4, 128, 16, [1, 40], [600, 1090], seed=12)
     g, pa = c.gpu(), c.plan()

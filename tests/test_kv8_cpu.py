@@ -136,7 +136,8 @@ def test_short_decode_sequences_stay_whole(count, top, whole, co):
 
 
 @pytest.mark.parametrize("n,ls,cut", [((64,), (4000,), True), ((2,), (300,), False), ((2,), (448,), False), ((2,), (449,), True), ((64, 3), (64, 2500), True),
-                                      ((64, 1, 200), (4000, 900, 210), True), ((3000,), (3000,), False), ((200,) * 5, (3000,) * 5, False)])
+                                      ((64, 1, 200), (4000, 900, 210), True), ((3000,), (3000,), False), ((200,) * 5, (3000,) * 5, False),
+                                      ((170,) * 7, (6170,) * 7, True), ((1200,), (5200,), True), ((2048,), (2048,), False)])
 def test_few_prefill_tiles_are_cut_along_their_keys(n, ls, cut):
     """Pieces of a tile are disjoint, in order and cover its keys; slots are
     those of the workspace, one after another; work-groups stay within the units."""
@@ -152,7 +153,8 @@ def test_few_prefill_tiles_are_cut_along_their_keys(n, ls, cut):
     assert bool(pieces) == cut
     if not cut:
         return
-    assert info["workspace_bytes"] > 0 and len(items) * info["prefill_grid_y"] <= info["cus_prefill"]
+    slots = info["cus_prefill"] * (1 if 2 * sum(-(-x * 7 // 128) for x in n if x > 1) * 4 <= info["cus_prefill"] else 3)
+    assert info["workspace_bytes"] > 0 and len(items) * info["prefill_grid_y"] <= slots
     for tile in {tuple(it[:4]) for it in pieces}:
         own = sorted((it for it in pieces if tuple(it[:4]) == tile), key=lambda it: it[5])
         s, _, _, r1 = tile
