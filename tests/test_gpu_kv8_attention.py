@@ -283,6 +283,20 @@ def test_prefill_crosses_a_block_table_window():
     c.check(*c.run(), "window")
 
 
+@pytest.mark.parametrize("hq,hkv,d,P,n,L,whole", [
+    (4, 1, 64, 16, 70, 8230, True), (4, 1, 64, 16, 30, 16500, False), (16, 1, 128, 16, 5, 8195, True), (16, 1, 128, 16, 40, 8200, True),
+    (4, 1, 64, 64, 30, 16450, False), (4, 1, 64, 16, 30, 8230, True), (4, 1, 64, 64, 70, 16450, True)])
+def test_whole_tiles_cross_block_table_windows(hq, hkv, d, P, n, L, whole):
+    """512 entries of pages of 16, 256 of 64: tiles left whole (plans for one
+    compute unit), by one key group and by two, end in a later window; long
+    pieces of cut ones too."""
+    c = Case(hq, hkv, d, P, [n], [L], seed=9)
+    tiles = -(-n * (hq // hkv) // 128)
+    pa = c.plan(cus_total=1)
+    assert (pa.plan.info["n_prefill_items"] == tiles) == whole
+    c.check(*c.run("prefill", pa=pa), "windows")
+
+
 def test_strided_cache():
     """K and V interleaved in one pool with gaps, block-table rows wider than the plan's."""
     c = Case(28, 4, 128, 16, [1, 30, 1], [100, 60, 500], seed=8, width=3)
