@@ -577,7 +577,12 @@ extern "C" int flex_attn_corun_create(int32_t cus_prefill, int32_t cus_decode, f
   }
   if ((e = hipExtStreamCreateWithCUMask(&c->prefill, words, mask_p)) != hipSuccess ||
       (e = hipExtStreamCreateWithCUMask(&c->decode, words, mask_d)) != hipSuccess ||
-      (e = hipMemset(c->flags, 0, 3 * sizeof(uint64_t))) != hipSuccess ||
+      // The counters are cleared before the pair is returned: hipMemset returns
+      // with the device's work still queued on the default stream, and a clear
+      // that ran behind the first step's writes would leave its waits without
+      // an end (and what an earlier pair counted would end them too soon).
+      (e = hipMemsetAsync(c->flags, 0, 3 * sizeof(uint64_t), c->prefill)) != hipSuccess ||
+      (e = hipStreamSynchronize(c->prefill)) != hipSuccess ||
       (e = hipEventCreateWithFlags(&c->join_ev[0], hipEventDisableTiming)) != hipSuccess ||
       (e = hipEventCreateWithFlags(&c->join_ev[1], hipEventDisableTiming)) != hipSuccess) {
     const int st = hip_fail(e, "co-run stream creation");
