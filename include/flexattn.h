@@ -258,7 +258,9 @@ int flex_attn_plan_info_get(const flex_attn_plan_t* plan, flex_attn_plan_info* o
 int flex_attn_plan_export(const flex_attn_plan_t* plan, int32_t* h_dst, size_t n_words);
 
 /* Enqueue an H2D copy of the plan words into device buffer d_dst of
- * dst_bytes >= device_plan_bytes on stream. The plan must outlive the copy. */
+ * dst_bytes >= device_plan_bytes on stream. The plan must outlive the copy,
+ * and a run call on another stream must wait for it: the kernels take their
+ * work from these words. */
 int flex_attn_plan_upload(const flex_attn_plan_t* plan, void* d_dst, size_t dst_bytes, void* stream);
 
 void flex_attn_plan_destroy(flex_attn_plan_t* plan);

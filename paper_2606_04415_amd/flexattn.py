@@ -863,7 +863,9 @@ class PagedAttention:
 
     ``inputs`` holds the device tensors: q, k_cache, v_cache (or None when V
     aliases K), block_table, seq_lens, query_start_loc (int32). ``run`` calls
-    the library on the current torch stream.
+    the library on the current torch stream. The plan is copied to the device
+    on the stream that is current at construction: a run on another stream has
+    to wait for that one first.
     """
 
     def __init__(self, shape: Shape, opts: Optional[PlanOpts], h_query_start_loc, h_seq_lens,
