@@ -864,7 +864,7 @@ class PagedAttention:
     ``inputs`` holds the device tensors: q, k_cache, v_cache (or None when V
     aliases K), block_table, seq_lens, query_start_loc (int32). ``run`` calls
     the library on the current torch stream. The plan is copied to the device
-    on the stream that is current at construction: a run on another stream has
+    on its stream that is current at construction: a run on another stream has
     to wait for that one first.
     """
 
@@ -876,7 +876,8 @@ class PagedAttention:
         info = self.plan.info
         self.d_plan = torch.empty(max(256, info["device_plan_bytes"]), dtype=torch.uint8, device=device)
         self.workspace = torch.empty(max(256, info["workspace_bytes"]), dtype=torch.uint8, device=device)
-        flex_attn_plan_upload(self.plan, self.d_plan)
+        with torch.cuda.device(self.d_plan.device):
+            flex_attn_plan_upload(self.plan, self.d_plan)
 
     def args(self, q, k_cache, v_cache, block_table, seq_lens, query_start_loc, out, lse=None) -> Args:
         return make_args(q, k_cache, v_cache, block_table, seq_lens, query_start_loc, out, lse,

@@ -412,3 +412,22 @@ def test_binding_refuses_cpu_tensors_and_other_shapes():
         F.make_kv8_args(t["q"], t["k"], t["v"], t["s"], t["bt"], t["ls"], t["qsl"], t["out"], torch.zeros(3, 27))
     with pytest.raises(ValueError, match="as many sequences"):
         F.make_kv8_args(t["q"], t["k"], t["v"], t["s"], t["bt"], t["ls"], t["qsl"][:2], t["out"])
+
+
+def test_a_plan_is_copied_on_its_own_device(monkeypatch):
+    """The upload goes to the stream of the device that holds the plan's copy,
+    which is the one that the run calls take, whatever device is current."""
+    import contextlib
+    seen = []
+
+    @contextlib.contextmanager
+    def on(dev):
+        seen.append(("enter", dev))
+        yield
+        seen.append(("leave", dev))
+
+    monkeypatch.setattr(torch.cuda, "device", on)
+    monkeypatch.setattr(F, "flex_attn_plan_upload", lambda plan, d_plan, stream=None: seen.append(("copy", d_plan.device)))
+    F.PagedAttention(F.make_shape(28, 4, 128, 128, 16, 0.1), F.make_opts(kv_bits=8), [0, 1], [40], 3, device="cpu")
+    dev = torch.device("cpu")
+    assert seen == [("enter", dev), ("copy", dev), ("leave", dev)]
