@@ -244,8 +244,10 @@ void prefill_kv8_kernel(AttnParams p) {
   // scheduling barriers. A wave's products go before the other waves' vector
   // work, which then fills the gaps of the matrix pipe (28/4 heads of 128, us: a
   // prompt of 2048 on 4096 keys 190.8 without and 186.2, of 2048 56.7 and 54.7,
-  // eight of 2048 286.3 and 284.2; heads of 64 alike; the softmax first instead
-  // 194 and 56.6, 288).
+  // eight of 2048 286.3 and 284.2; the softmax first instead 194, 56.6 and 288).
+  // Heads of 64, with half the products, keep the turn up to the maxima (32/8:
+  // 2048 on 4096 keys 128.1 and 125.5, 7 of 170 on 6000 110.7 and 107.0, eight
+  // of 2048 192.6 and 190.8; with heads of 128 16 of 300 on 300 55.0 and 58.3).
   auto compute_tile = [&](bool masked, int st, int kc0, auto&& scored) {
     const uint32_t stage = uint32_t(__builtin_amdgcn_readfirstlane(region + uint32_t(st * L::STAGE)));
     const uint32_t k_at = stage + k_off, v_at = stage + v_off;
@@ -266,7 +268,7 @@ void prefill_kv8_kernel(AttnParams p) {
         __builtin_amdgcn_sched_barrier(0);
       }
     }
-    __builtin_amdgcn_s_setprio(0);
+    if constexpr (D == 128) __builtin_amdgcn_s_setprio(0);
     scored();
     u32x4 vb[VD];
 #pragma unroll
@@ -283,6 +285,7 @@ void prefill_kv8_kernel(AttnParams p) {
     for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
     mx = swap32_combine_max(mx) * p.scale_log2;
 
+    if constexpr (D == 64) __builtin_amdgcn_s_setprio(0);
     // Lazy rescale: a row's maximum moves only when the tile's exceeds it by
     // more than the threshold.
     const bool need = mx > m + kRescaleThreshold;
