@@ -19,10 +19,10 @@
 //  - A tile's keys may be cut into pieces (plan.cpp); merge_tiles_kernel joins
 //    them.
 //
-// Measured: eight prompts of 2048, 28/4 heads of 128, 284 us, 847 TFLOP/s. With the machine full the clock gives way: against
-// 16x16x32 it takes 6% fewer clocks and 2% more time, at 2.1 GHz instead of
-// 2.25, and vector work, operand reads and products each fill less than two
-// thirds of the clocks.
+// Measured: eight prompts of 2048, 28/4 heads of 128, 284 us, 847 TFLOP/s. With
+// the machine full the clock gives way: against 16x16x32 it takes 6% fewer
+// clocks and 2% more time, at 2.1 GHz instead of 2.25, and vector work, operand
+// reads and products each fill less than two thirds of the clocks.
 #include <float.h>
 #include <hip/hip_runtime.h>
 
