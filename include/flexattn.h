@@ -497,8 +497,10 @@ int flex_attn_rope_append(const flex_attn_shape* shape, const flex_attn_rope* ro
  * The new tokens are the batch's, as the attention calls take it: sequence s
  * has tokens query_start_loc[s] .. query_start_loc[s + 1] - 1 of the new rows
  * and holds seq_lens[s] tokens after the call, in the pages of its
- * block_table row. Rows of k_new, v_new, q and q_out past
- * query_start_loc[num_seqs] (padding) are neither read nor written.
+ * block_table row. query_start_loc does not decrease; it may start above 0 (a
+ * part of a larger batch's). Rows of k_new, v_new, q and q_out before
+ * query_start_loc[0] and from query_start_loc[num_seqs] on (padding) are
+ * neither read nor written.
  *
  * Per block with new rows, KV head and K / V: with a the largest magnitude
  * among the new rows' finite values, the scale is the least 2^k, k >= -117,

@@ -320,8 +320,9 @@ __global__ __launch_bounds__(512) void rope_append_kernel(RopeAppendParams p) {
 // ---------------------------------------------------------------------------
 
 // The sequence that holds new token t: the largest s with query_start_loc[s]
-// <= t (B: none, padding), its first and end token and its length. 63 probes at
-// a time; the last round, over 64 neighbours, brings the rest along.
+// <= t (0 also where there is none, B behind the last), its first and end token
+// and its length. 63 probes at a time; the last round, over 64 neighbours,
+// brings the rest along. No sequence holds a token outside [start, end).
 struct Sequence {
   int s, start, end, L;
 };
@@ -477,7 +478,10 @@ __global__ __launch_bounds__(64 * kAppendWaves) void kv8_append_kernel(Kv8Append
   Positions<AXES> x;
   if (rope && p.rope.positions) x = read_positions<AXES>(p.rope, t);
   const Sequence q = find_sequence(p.qsl, p.seq_lens, p.num_seqs, t, lane);
-  if (q.s >= p.num_seqs) return;         // padding token
+  // Padding: behind the last sequence or before the first one. (The token's rank
+  // among its block's new rows, below, is the first head that it takes: negative
+  // for a token before its sequence's first.)
+  if (q.s >= p.num_seqs || t < q.start || t >= q.end) return;
   const int64_t q1 = min(int64_t(q.end), p.n_tokens);
   const int32_t pos = int32_t(q.L - (q.end - t));
   if (rope && !p.rope.positions) x = position_at<AXES>(p.rope, pos);
@@ -500,8 +504,7 @@ __global__ __launch_bounds__(64 * kAppendWaves) void kv8_append_kernel(Kv8Append
   const int32_t first = max(pos & ~15, q.L - (q.end - max(q.start, 0)));   // position of the block's first new row
   const int r0 = first & 15, rank = pos - first;
   const int64_t tf = t - rank;
-  const int count = int(min(int64_t(16 - r0), q1 - tf));
-  if (count < 1) return;   // (query_start_loc out of order)
+  const int count = int(min(int64_t(16 - r0), q1 - tf));   // at least rank + 1
   const int64_t row0 = pos & (p.P - 1) & ~15;         // the block's first slot in its page
   const auto read = [&](auto& b, int h, int kv) {
     b.read(p, rope && !kv, (kv ? p.v_new : p.k_new) + h * D, kv ? p.v_new_stride : p.k_new_stride, tf, first, count, lane);

@@ -209,6 +209,28 @@ def test_tokens_past_the_calls_are_left_out():
     assert not np.array_equal(got[c.bt[1, 1], :3], c.codes[0][c.bt[1, 1], :3])
 
 
+@pytest.mark.parametrize("geo,ns,ls,first", [
+    (QWEN, [5, 1, 20, 1], [5, 40, 33, 17], 1), (QWEN, [3, 2, 1], [3, 16, 100], 2), (ONE, [9, 30], [9, 64], 1),
+    (D64, [1] * 80 + [7], [20] * 80 + [50], 70), (ONE, [4200, 40, 3], [4200, 41, 19], 1)])
+@pytest.mark.parametrize("rope", [True, False])
+def test_tokens_before_the_first_sequence_are_padding(geo, ns, ls, first, rope):
+    """A part of a batch, its query_start_loc starting above 0: the tokens of the
+    sequences left out are no one's. Nothing of theirs is written, nothing counted."""
+    log(f"kv8 append {geo}: sequences from {first} of {len(ns)}, rope {rope}")
+    c = Case(geo, ns, ls, seed=13, rope=rope, pad=2, max_pos=8192)
+    c.bt, c.ls, c.qsl = c.bt[first:].copy(), c.ls[first:].copy(), c.qsl[first:].copy()
+    g = c.run()
+    torch.cuda.synchronize()
+    assert int(g["bad"].item()) == 0
+    want = c.reference()
+    for n, ref in zip(("kc", "vc", "sc"), want):
+        got = g[n].view(torch.uint8).cpu().numpy()
+        assert np.array_equal(got, ref), f"{n} differs in {(got != ref).sum()} of {ref.size} bytes"
+    if rope:
+        q, t0, t1 = g["q_out"].cpu(), int(c.qsl[0]), int(c.qsl[-1])
+        assert (q[:t0] == 7.0).all() and (q[t1:] == 7.0).all() and (q[t0:t1] != 7.0).any(-1).any(-1).all()
+
+
 def test_strided_caches_and_rows():
     """A cache that is part of a larger one (both of K and V, other layers'
     pages between) and rows of one projection: the gaps keep their bytes."""
