@@ -426,6 +426,10 @@ struct Block {
   // byte. The new rows are r0, r0 + 1, ..; earlier rows of the sequence are
   // there iff r0 > 0.
   __device__ __forceinline__ void write(uint8_t* codes, int64_t ss, uint8_t* scale, int r0, int lane) const {
+    bool any = false;
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i) any = any || mine[i];
+    if (__builtin_amdgcn_ballot_w64(any) == 0) return;   // all rows skipped: the block keeps its scale too
     const int old = r0 > 0 ? int(*scale) - 127 : -128;
     uint32_t top = 0;
 #pragma unroll

@@ -197,6 +197,21 @@ def test_bad_pages_and_positions_are_skipped_and_counted():
     assert (q[skipped] == 7.0).all() and (q[[1, 16, 33, 42]] != 7.0).any(-1).any(-1).all()
 
 
+@pytest.mark.parametrize("geo", [QWEN, ONE])
+@pytest.mark.parametrize("ns,ls", [([1, 1], [17, 1]), ([3, 16, 1], [19, 16, 20]), ([20, 2], [36, 40])])
+def test_a_block_of_skipped_tokens_keeps_its_scale(geo, ns, ls):
+    """Every token's position is outside the table: codes, scales and queries stay
+    as they are, in blocks whose first row is among the tokens as in others."""
+    c = Case(geo, ns, ls, seed=4, positions=True)
+    c.pos[:] = np.where(np.arange(c.n) % 2, -1, c.max_pos)[None]
+    g = c.run()
+    torch.cuda.synchronize()
+    assert int(g["bad"].item()) == c.n
+    for n, was in zip(("kc", "vc", "sc"), c.codes):
+        assert np.array_equal(g[n].view(torch.uint8).cpu().numpy(), was), n
+    assert (g["q_out"].cpu() == 7.0).all()
+
+
 def test_tokens_past_the_calls_are_left_out():
     """n_tokens below query_start_loc's end: the tokens past it are not appended."""
     c = Case(QWEN, [1, 30], [9, 30], seed=7, rope=False)
