@@ -453,7 +453,10 @@ struct Block {
         *at = v;
       }
     }
-    const float inv = __uint_as_float(uint32_t(max(127 - k, 1)) << 23);
+    // 2^-k. (The append's own scales end at k = 120; a block that a caller
+    // filled may hold 2^127 or NaN, whose inverses, 2^-128 for the latter, are
+    // subnormal.)
+    const float inv = __uint_as_float(k < 127 ? uint32_t(127 - k) << 23 : 0x400000u >> (k - 127));
 #pragma unroll
     for (int i = 0; i < PASSES; ++i) {
       if (!mine[i]) continue;

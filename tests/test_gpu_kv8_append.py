@@ -175,6 +175,20 @@ def test_exact_powers_and_the_largest_code():
     assert [int(sc[c.bt[i, 0], 0, 0, 0]) for i in range(4)] == [127, 128, 127, 10]
 
 
+@pytest.mark.parametrize("geo", [QWEN, D64])
+def test_every_scale_byte_that_a_block_can_have(geo):
+    """A block that holds a row takes one more, at each of the 256 scale bytes:
+    those that an empty cache has or that the append writes, and the rest. New
+    rows from tiny to the type's largest."""
+    for size in (2.0 ** -100, 1.0, 2.0 ** 126):
+        c = Case(geo, [1] * 256, [2 + i % 15 for i in range(256)], seed=6, rope=False)
+        c.k = (c.k.float().clamp(-2, 2) / 2 * size).to(torch.bfloat16)
+        c.v = (c.v.float().clamp(-2, 2) / 2 * size).to(torch.bfloat16)
+        for s in range(256):
+            c.codes[2][c.bt[s, 0], 0] = s
+        c.check(c.run(), f"rows of {size:g}")
+
+
 def test_bad_pages_and_positions_are_skipped_and_counted():
     c = Case(QWEN, [1, 40, 1, 1], [30, 40, 5, 50], seed=4, positions=True)
     good = c.reference()
