@@ -482,10 +482,15 @@ int flex_attn_rope_append(const flex_attn_shape* shape, const flex_attn_rope* ro
  * k_cache and v_cache hold e4m3 codes (OCP, 0x7F and 0xFF are NaN) in the
  * bf16 caches' layout, strides in bytes. Each block of 16 tokens of a page
  * has, for each KV head, one scale for its keys and one for its values: a byte
- * b that stands for 2^(b - 127) (e8m0; 255 is NaN, 0 is taken as 0). A cached
- * value is code * scale. Scales are powers of two because the matrix-core
- * operands are bf16: a scaled code is then a bf16 value exactly, so attention
- * over the cache loses nothing beyond the one rounding of the append.
+ * b that stands for 2^(b - 127) (e8m0: 0 is 2^-127, 255 is NaN; the append
+ * writes 10 to 247). A cached value is code * scale. Scales are powers of two
+ * because the matrix-core operands are bf16: a scaled code is then a bf16 value
+ * exactly, so attention over the cache loses nothing beyond the one rounding of
+ * the append. (Below 2^-126, which takes a byte under 10, it is rounded to a
+ * subnormal bf16 value; from 2^128 on, to which the append rounds a bf16 value
+ * of 248 * 2^120 or more, it is infinite. As over a bf16 cache, an infinite
+ * value counts as NaN for the queries that it is masked for, and weighted sums
+ * of values are fp32 before their division: those that reach 2^128 are infinite.)
  *  kv_scales  bytes [num_pages][page_size / 16][Hkv][2] (key, value): page p
  *             starts at byte p * scale_page_stride, the rest is contiguous;
  *             base and stride are multiples of 2 bytes.

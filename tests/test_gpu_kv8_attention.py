@@ -175,6 +175,27 @@ def test_all_codes_and_scales_reach_the_output():
     assert torch.equal(out.float(), want)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n,ks", [(1, list(range(0, 10)) + list(range(240, 255))), (2, list(range(0, 10)) + list(range(240, 246)))])
+def test_scale_bytes_at_the_ends(d, n, ks):
+    """Bytes that the append does not write, or only for the largest values: byte
+    0 is 2^-127, tiny values are subnormal ones, values from 2^128 on infinite. n
+    new tokens with like keys and values (one: decode, two: prefill, whose
+    second sums two halves)."""
+    hkv = 256 // d
+    c = Case(hkv, hkv, d, 16, [n] * len(ks), [n] * len(ks), seed=1)
+    row = np.array([x for x in range(256) if (x & 127) != 127], dtype=np.uint8)
+    for s, b in enumerate(ks):
+        c.k[c.bt[s, 0], :n] = 0
+        c.v[c.bt[s, 0], :n] = np.concatenate([row, row[:2]]).reshape(hkv, d)
+        c.s[c.bt[s, 0], 0, :, 1] = b
+    out, _ = c.run()
+    v = c.values()[1]
+    want = torch.from_numpy(np.repeat(np.stack([v[c.bt[s, 0], 0] for s in range(len(ks))]), n, 0)).float().to(torch.bfloat16)
+    assert not want.isnan().any() and (want.isinf().any() if n == 1 else want.isfinite().all())
+    assert torch.equal(out, want)
+
+
 def test_nan_reaches_only_what_attends_it():
     """A NaN value row (a key's, a whole block's by its scale) makes the rows that
     attend it NaN in its columns and leaves other sequences alone."""
