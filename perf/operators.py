@@ -475,9 +475,12 @@ def run(state):
         F.flex_attn_decode_kv8(plan, args)
     elif case["call"] == "prefill":
         F.flex_attn_prefill_kv8(plan, args)
-    elif case["call"] == "corun":
+    elif case["call"] == "corun":   # behind what the caller's stream holds, and before what follows there
+        caller = torch.cuda.current_stream()
+        _stream.wait_stream(caller)
         with torch.cuda.stream(_stream):
             F.flex_attn_mixed_kv8(plan, args, F.FLEX_MODE_CORUN, corun=state["corun"])
+        caller.wait_stream(_stream)
     else:
         F.flex_attn_mixed_kv8(plan, args, F.FLEX_MODE_SERIAL)
     return {"out": state["out"], "lse": state["lse"]} if case["lse"] else state["out"]
