@@ -270,7 +270,8 @@ def _scale(case):
 
 
 _stream = None   # the program's own stream: co-run steps are issued from it
-_pair = {}       # the one co-run pair a program keeps, by its split
+_pair = {}       # the one co-run pair a program keeps, by its split (a state asks for it at each pass:
+                 # a state of another split may have replaced it)
 
 
 def _corun(F, cus_prefill, cus_decode):
@@ -304,9 +305,11 @@ def _prepare_own(state):
         bt, sl, qsl = x["h"]
         pa = F.PagedAttention(shape, F.make_opts(cus_decode=case["cus_decode"], kv_bits=8), qsl, sl, bt.shape[1])
         out, lse = pa.alloc_out(x["q"], with_lse=case["lse"])
-        corun = _corun(F, pa.plan.info["cus_prefill"], pa.plan.info["cus_decode"]) if case["call"] == "corun" else None
+        split = pa.plan.info["cus_prefill"], pa.plan.info["cus_decode"]
+        if case["call"] == "corun":
+            _corun(F, *split)
         args = pa.kv8_args(x["q"], x["k"], x["v"], x["scales"], x["bt"], x["sl"], x["qsl"], out, lse)
-        state.update(pa=pa, args=args, corun=corun, out=out, lse=lse)
+        state.update(pa=pa, args=args, split=split, out=out, lse=lse)
         return state
     rope = None
     if case["rot_dim"]:
@@ -479,7 +482,7 @@ def run(state):
         caller = torch.cuda.current_stream()
         _stream.wait_stream(caller)
         with torch.cuda.stream(_stream):
-            F.flex_attn_mixed_kv8(plan, args, F.FLEX_MODE_CORUN, corun=state["corun"])
+            F.flex_attn_mixed_kv8(plan, args, F.FLEX_MODE_CORUN, corun=_corun(F, *state["split"]))
         caller.wait_stream(_stream)
     else:
         F.flex_attn_mixed_kv8(plan, args, F.FLEX_MODE_SERIAL)
