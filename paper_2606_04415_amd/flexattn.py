@@ -399,18 +399,52 @@ def flex_attn_plan_upload(plan: Plan, d_plan, stream=None):
                                       d_plan.numel() * d_plan.element_size(), s), "flex_attn_plan_upload")
 
 
+class _PlanCopy:
+    """A plan's copy to the device, which is queued on the stream that is current here:
+    a run on another stream waits for it, the first time."""
+
+    def __init__(self, device):
+        import torch
+        self.device, self.event = device, None
+        if device.type != "cuda" or torch.cuda.is_current_stream_capturing():   # (in a graph: its own order)
+            return
+        s = torch.cuda.current_stream(device)
+        self.event, self.behind = s.record_event(), {s.cuda_stream}
+
+    def order(self, stream):
+        import torch
+        if self.event is None:
+            return
+        handle = getattr(stream, "value", stream) or 0
+        if handle in self.behind:
+            return
+        s = torch.cuda.ExternalStream(handle, device=self.device)
+        with torch.cuda.stream(s):
+            if torch.cuda.is_current_stream_capturing():   # a capture may not wait for what is outside of it
+                return
+        s.wait_event(self.event)
+        self.behind.add(handle)
+
+
+def _behind_plan_copy(args, stream):
+    copy = getattr(args, "plan_copy", None)
+    if copy is not None:
+        copy.order(stream)
+    return stream
+
+
 def flex_attn_decode(plan: Plan, args: Args, stream=None):
-    s = stream if stream is not None else current_stream()
+    s = _behind_plan_copy(args, stream if stream is not None else current_stream())
     check(lib().flex_attn_decode(plan.handle, ctypes.byref(args), s), "flex_attn_decode")
 
 
 def flex_attn_prefill(plan: Plan, args: Args, stream=None):
-    s = stream if stream is not None else current_stream()
+    s = _behind_plan_copy(args, stream if stream is not None else current_stream())
     check(lib().flex_attn_prefill(plan.handle, ctypes.byref(args), s), "flex_attn_prefill")
 
 
 def flex_attn_mixed(plan: Plan, args: Args, mode: int, stream=None, corun: "Corun" = None):
-    s = stream if stream is not None else current_stream()
+    s = _behind_plan_copy(args, stream if stream is not None else current_stream())
     check(lib().flex_attn_mixed(plan.handle, ctypes.byref(args), mode, s,
                                 corun.handle if corun is not None else None), "flex_attn_mixed")
 
@@ -437,7 +471,7 @@ def set_debug(level: int) -> int:
 
 def flex_attn_mixed_static(plan: Plan, args: Args, mode: int, stream=None, corun: "Corun" = None):
     """flex_attn_mixed with the split-K partials in the library's fixed scratch (allocates nothing)."""
-    s = stream if stream is not None else current_stream()
+    s = _behind_plan_copy(args, stream if stream is not None else current_stream())
     check(lib().flex_attn_mixed_static(plan.handle, ctypes.byref(args), mode, s,
                                        corun.handle if corun is not None else None), "flex_attn_mixed_static")
 
@@ -502,10 +536,12 @@ def _run(what, args, stream, *call, last=()):
     if dev.type != "cuda":
         raise ValueError(f"{what} needs GPU tensors, not {dev}")
     if dev.index == torch.cuda.current_device():
-        st = getattr(lib(), what)(*call, stream if stream is not None else current_stream(), *last)
+        s = _behind_plan_copy(args, stream if stream is not None else current_stream())
+        st = getattr(lib(), what)(*call, s, *last)
     else:
         with torch.cuda.device(dev):
-            st = getattr(lib(), what)(*call, stream if stream is not None else current_stream(), *last)
+            s = _behind_plan_copy(args, stream if stream is not None else current_stream())
+            st = getattr(lib(), what)(*call, s, *last)
     if st != FLEX_OK:
         check(st, what)
 
@@ -864,8 +900,9 @@ class PagedAttention:
     ``inputs`` holds the device tensors: q, k_cache, v_cache (or None when V
     aliases K), block_table, seq_lens, query_start_loc (int32). ``run`` calls
     the library on the current torch stream. The plan is copied to the device
-    on its stream that is current at construction: a run on another stream has
-    to wait for that one first.
+    on its stream that is current at construction; a run on another stream
+    with arguments made here waits for the copy (but in a capture, which cannot:
+    there it has to be over).
     """
 
     def __init__(self, shape: Shape, opts: Optional[PlanOpts], h_query_start_loc, h_seq_lens,
@@ -878,15 +915,20 @@ class PagedAttention:
         self.workspace = torch.empty(max(256, info["workspace_bytes"]), dtype=torch.uint8, device=device)
         with torch.cuda.device(self.d_plan.device):
             flex_attn_plan_upload(self.plan, self.d_plan)
+            self.plan_copy = _PlanCopy(self.d_plan.device)
 
     def args(self, q, k_cache, v_cache, block_table, seq_lens, query_start_loc, out, lse=None) -> Args:
-        return make_args(q, k_cache, v_cache, block_table, seq_lens, query_start_loc, out, lse,
-                         self.d_plan, self.workspace)
+        a = make_args(q, k_cache, v_cache, block_table, seq_lens, query_start_loc, out, lse,
+                      self.d_plan, self.workspace)
+        a.plan_copy = self.plan_copy
+        return a
 
     def kv8_args(self, q, k_cache, v_cache, kv_scales, block_table, seq_lens, query_start_loc, out, lse=None) -> Kv8Args:
         """Arguments of the calls over an 8-bit cache (a plan made with kv_bits=8)."""
-        return make_kv8_args(q, k_cache, v_cache, kv_scales, block_table, seq_lens, query_start_loc, out, lse,
-                             self.d_plan, self.workspace)
+        a = make_kv8_args(q, k_cache, v_cache, kv_scales, block_table, seq_lens, query_start_loc, out, lse,
+                          self.d_plan, self.workspace)
+        a.plan_copy = self.plan_copy
+        return a
 
     def alloc_out(self, q, with_lse=False):
         import torch

@@ -431,3 +431,72 @@ def test_a_plan_is_copied_on_its_own_device(monkeypatch):
     F.PagedAttention(F.make_shape(28, 4, 128, 128, 16, 0.1), F.make_opts(kv_bits=8), [0, 1], [40], 3, device="cpu")
     dev = torch.device("cpu")
     assert seen == [("enter", dev), ("copy", dev), ("leave", dev)]
+
+
+class _Stream:
+    """A stream of torch's, by its handle; what is done with it is logged."""
+    def __init__(self, handle, log, device=None):
+        self.cuda_stream, self.log = handle, log
+
+    def record_event(self):
+        self.log.append(("record", self.cuda_stream))
+        return "the copy's event"
+
+    def wait_event(self, event):
+        self.log.append(("wait", self.cuda_stream, event))
+
+
+def test_a_run_on_another_stream_waits_for_the_plans_copy(monkeypatch):
+    """Every run call, once a stream: not on the stream that the copy is queued
+    on, and not in a capture."""
+    import contextlib
+    log, capturing = [], [False]
+    monkeypatch.setattr(torch.cuda, "device", lambda d: contextlib.nullcontext())
+    monkeypatch.setattr(torch.cuda, "stream", lambda s: contextlib.nullcontext())
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda d=None: _Stream(5, log))
+    monkeypatch.setattr(torch.cuda, "ExternalStream", lambda h, device=None: _Stream(h, log))
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: capturing[0])
+    copy = F._PlanCopy(torch.device("cuda:0"))
+    assert log == [("record", 5)]
+
+    class Lib:
+        def __getattr__(self, name):
+            return lambda *a: log.append(name) or F.FLEX_OK
+
+    monkeypatch.setattr(F, "lib", lambda: Lib())
+    t = tensors()
+    a = F.make_kv8_args(t["q"], t["k"], t["v"], t["s"], t["bt"], t["ls"], t["qsl"], t["out"])
+    a.device, a.plan_copy = torch.device("cuda:0"), copy
+
+    class P:
+        handle, shape, batch = None, SHAPE, (2, 3)
+
+    a16 = F.Args()
+    a16.plan_copy = copy
+    calls = [(F.flex_attn_decode, (P, a16)), (F.flex_attn_prefill, (P, a16)), (F.flex_attn_mixed, (P, a16, 0)),
+             (F.flex_attn_mixed_static, (P, a16, 0)), (F.flex_attn_decode_kv8, (P, a)), (F.flex_attn_prefill_kv8, (P, a)),
+             (F.flex_attn_mixed_kv8, (P, a, 0))]
+    for i, (call, args) in enumerate(calls):
+        name, side, null = call.__name__, 100 + i, ctypes.c_void_p(200 + i)
+        del log[:]
+        call(*args)
+        call(*args, stream=5)
+        assert log == [name, name], name                       # the copy's own stream
+        capturing[0] = True
+        call(*args, stream=side)
+        capturing[0] = False
+        assert log[2:] == [name], name                         # a capture, which must not wait
+        call(*args, stream=side)
+        call(*args, stream=side)
+        call(*args, stream=null)
+        assert log[3:] == [("wait", side, "the copy's event"), name, name, ("wait", null.value, "the copy's event"), name], name
+    for shape, bits, make in ((SHAPE, 8, "kv8_args"), (SHAPE, 16, "args")):
+        monkeypatch.undo()
+        with monkeypatch.context() as m:
+            m.setattr(torch.cuda, "device", lambda d: contextlib.nullcontext())
+            m.setattr(F, "flex_attn_plan_upload", lambda plan, d_plan, stream=None: None)
+            pa = F.PagedAttention(shape, F.make_opts(kv_bits=bits), t["qsl"], t["ls"], 3, device="cpu")
+        kc = torch.zeros(t["k"].shape, dtype=torch.bfloat16)
+        cache = (t["k"], t["v"], t["s"]) if bits == 8 else (kc, kc)
+        assert getattr(pa, make)(t["q"], *cache, t["bt"], t["ls"], t["qsl"], t["out"]).plan_copy is pa.plan_copy
