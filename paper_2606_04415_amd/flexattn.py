@@ -586,7 +586,8 @@ def make_rope(cos_sin, positions=None, rot_begin: int = 0, neighbours: bool = Fa
     """Rope from device tensors: cos_sin fp32 [max_position, rot_dim] (rope_table),
     positions int32 [tokens] or [axes, tokens] (rows may be apart), or None for
     flex_attn_kv8_append with one axis. sections: pairs of each axis, given
-    when there is more than one."""
+    when there is more than one. (This one, like the arguments of the calls that
+    rotate or use an 8-bit cache, keeps its tensors.)"""
     import torch
     _require(cos_sin.dtype == torch.float32, f"cos_sin must be float32, not {cos_sin.dtype}")
     _require(cos_sin.dim() == 2 and cos_sin.is_contiguous(), "cos_sin must be [max_position, rot_dim], contiguous")
@@ -607,6 +608,7 @@ def make_rope(cos_sin, positions=None, rot_begin: int = 0, neighbours: bool = Fa
     for a, n in enumerate(axes):
         r.sections[a] = n
     r.device = _one_device([cos_sin, positions])
+    r.tensors = (cos_sin, positions)
     return r
 
 
@@ -639,7 +641,8 @@ def make_rope_append_args(q, q_out, k_new, v_new, slot_mapping, k_cache, v_cache
     _require(k_new.shape[0] == n and (v_new is None or v_new.shape[0] == n), "q, k_new and v_new must have the same tokens")
     if bad_count is not None:
         a.kv.bad_count = _index("bad_count", bad_count)
-    a.device = _one_device([q, q_out, k_new, v_new, slot_mapping, k_cache, v_cache, bad_count])
+    a.tensors = (q, q_out, k_new, v_new, slot_mapping, k_cache, v_cache, bad_count)
+    a.device = _one_device(a.tensors)
     a.sizes = (Hq, Hkv, dk, None if v_new is None else v_cache.shape[3], k_cache.shape[1])
     return a
 
@@ -712,8 +715,8 @@ def make_kv8_append_args(k_new, v_new, block_table, seq_lens, query_start_loc, k
     a.k_cache, a.v_cache, a.kv_scales = k_cache.data_ptr(), v_cache.data_ptr(), kv_scales.data_ptr()
     if bad_count is not None:
         a.bad_count = _index("bad_count", bad_count)
-    a.device = _one_device([k_new, v_new, block_table, seq_lens, query_start_loc, k_cache, v_cache, kv_scales, q, q_out,
-                            bad_count])
+    a.tensors = (k_new, v_new, block_table, seq_lens, query_start_loc, k_cache, v_cache, kv_scales, q, q_out, bad_count)
+    a.device = _one_device(a.tensors)
     a.sizes = (Hq, heads, d, d, k_cache.shape[1])
     return a
 
@@ -737,7 +740,8 @@ def make_kv8_args(q, k_cache, v_cache, kv_scales, block_table, seq_lens, query_s
     a.attn.k_cache, a.attn.v_cache, a.attn.k_stride, a.attn.v_stride = k_cache.data_ptr(), v_cache.data_ptr(), ks, vs
     a.attn.num_pages = k_cache.shape[0]
     a.kv_scales = kv_scales.data_ptr()
-    a.device = _one_device([q, k_cache, v_cache, kv_scales, lse, d_plan, workspace])
+    a.tensors = (q, k_cache, v_cache, kv_scales, block_table, seq_lens, query_start_loc, out, lse, d_plan, workspace)
+    a.device = _one_device(a.tensors)
     _require(q.dim() == 3, "q must be [tokens, Hq, d]")
     _require(out.shape[:2] == q.shape[:2] and out.shape[2:] == v_cache.shape[3:], "out must be [tokens, Hq, d]")
     _require(lse is None or lse.shape == q.shape[:2], "lse must be [tokens, Hq]")

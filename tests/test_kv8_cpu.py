@@ -414,6 +414,29 @@ def test_binding_refuses_cpu_tensors_and_other_shapes():
         F.make_kv8_args(t["q"], t["k"], t["v"], t["s"], t["bt"], t["ls"], t["qsl"][:2], t["out"])
 
 
+def test_arguments_keep_their_tensors():
+    """The calls read them by their addresses: a table made in place, or a view
+    that no one else holds, stays until the arguments go."""
+    import gc
+    import weakref
+    t = tensors()
+    kc = torch.zeros(4, 16, 4, 128, dtype=torch.bfloat16)
+    bad, lse, pos = torch.zeros(1, dtype=torch.int32), torch.zeros(3, 28), torch.zeros(3, dtype=torch.int32)
+    append = (t["k_new"], t["v_new"], t["bt"], t["ls"], t["qsl"], t["k"], t["v"], t["s"], t["q"], t["q_out"], bad)
+    for make, given in ((F.make_rope, (F.rope_table(64, 128, device="cpu"), pos)),
+                        (F.make_rope_append_args, (t["q"], t["q_out"], t["k_new"], t["v_new"], pos, kc, kc, bad)),
+                        (F.make_kv8_append_args, append),
+                        (F.make_kv8_args, (t["q"], t["k"], t["v"], t["s"], t["bt"], t["ls"], t["qsl"], t["out"], lse, bad, bad))):
+        views = [x[:] for x in given]
+        refs, a = [weakref.ref(x) for x in views], make(*views)
+        del views
+        gc.collect()
+        assert all(r() is not None for r in refs), make.__name__
+        del a
+        gc.collect()
+        assert not any(r() is not None for r in refs), make.__name__
+
+
 def test_a_plan_is_copied_on_its_own_device(monkeypatch):
     """The upload goes to the stream of the device that holds the plan's copy,
     which is the one that the run calls take, whatever device is current."""
