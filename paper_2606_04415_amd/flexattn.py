@@ -309,13 +309,14 @@ def flex_attn_plan(shape: Shape, opts: Optional[PlanOpts], query_start_loc: Sequ
     numpy arrays or CPU tensors. Raises FlexAttnError with the library's
     status on failure."""
     out = ctypes.c_void_p()
+    starts = _i32_array(query_start_loc)
     st = lib().flex_attn_plan(ctypes.byref(shape), ctypes.byref(opts) if opts is not None else None,
-                              len(seq_lens), _i32_array(query_start_loc), _i32_array(seq_lens),
+                              len(seq_lens), starts, _i32_array(seq_lens),
                               int(max_pages_per_seq), ctypes.byref(out))
     check(st, "flex_attn_plan")
     plan = Plan(out.value)
     plan.shape = Shape.from_buffer_copy(shape)
-    plan.batch = (len(seq_lens), int(query_start_loc[-1]))
+    plan.batch = (len(seq_lens), starts[len(seq_lens)])   # (the array may go on)
     return plan
 
 

@@ -414,6 +414,16 @@ def test_binding_refuses_cpu_tensors_and_other_shapes():
         F.make_kv8_args(t["q"], t["k"], t["v"], t["s"], t["bt"], t["ls"], t["qsl"][:2], t["out"])
 
 
+def test_plans_take_the_starts_that_the_batch_needs():
+    """query_start_loc may go on past the batch (a buffer of the largest one), be a
+    column, or be empty for an empty batch, as before plans knew their batch."""
+    for qsl, ls in (([0, 1, 4, 0, 0], [9, 8]), ([], []), (np.array([[0], [1], [4]]), [9, 8]),
+                    (torch.tensor([0, 1, 4, -7]), torch.tensor([9, 8]))):
+        for opts in (F.make_opts(kv_bits=8), None):
+            p = F.flex_attn_plan(SHAPE, opts, qsl, ls, 4)
+            assert p.batch == ((2, 4) if len(ls) else (0, 0)) and p.info["num_seqs"] == len(ls)
+
+
 def test_arguments_keep_their_tensors():
     """The calls read them by their addresses: a table made in place, or a view
     that no one else holds, stays until the arguments go."""
