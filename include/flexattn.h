@@ -84,7 +84,9 @@ typedef struct flex_attn_shape {
   int32_t v_aliases_k;
 } flex_attn_shape;
 
-/* Planner tunables; a zero field takes the default in brackets.
+/* Planner tunables; a zero field takes the default in brackets. Clear the whole
+ * structure before setting fields, and build with the header of the library
+ * that is called: fields are added at the end (kv_bits lies in what was padding).
  * cus_decode: CUs the decode phase is partitioned for and, in co-run mode,
  * runs on [0 = all]; -1 asks the cost model to choose the split among
  * multiples of split_granule from the rates below. */

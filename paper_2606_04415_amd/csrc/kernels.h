@@ -1,5 +1,5 @@
 // Kernel parameter blocks and launchers (host-callable, defined in attention.hip,
-// decode_kv8.hip, latent.hip and kv_append.hip).
+// decode_kv8.hip, prefill_kv8.hip, latent.hip and kv_append.hip).
 #pragma once
 
 #include <hip/hip_runtime.h>

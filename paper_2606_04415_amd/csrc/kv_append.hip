@@ -218,7 +218,7 @@ __device__ __forceinline__ void turn_unit(const RopeParams& r, const Turn& t, fl
 
 // Heads that one thread takes: it reads the cosines and sines of its unit once
 // for all of them, and their loads are in flight together. (1, 2 and 4 heads,
-// kernel times: 2176 tokens of 28/4 heads of 128 10.5, 9.9 and 9.9 us; 5900
+// kernel times: 2176 tokens of 28/4 heads of 128 10.5, 9.9 and 9.9 us; 5648
 // tokens of 32/8 heads of 64 on three axes 21.2, 18.4 and 20.0; a 4096-token
 // latent prompt 257, 242 and 240; 64 tokens 3.6, 4.0 and 4.9.)
 constexpr int kHeadsPerThread = 2;
@@ -315,8 +315,10 @@ __global__ __launch_bounds__(512) void rope_append_kernel(RopeAppendParams p) {
 // A wave holds its rows in registers between the maximum that gives the scale
 // and the conversion, so they are read once. (With all tasks of a block in the
 // work-group of its first token, a 2048-token chunk beside 128 decodes took
-// 33.6 us, now 13.3, 3 of them above the rotation into the bf16 cache: the
-// search, the page, the rows, their maximum and the codes follow each other.)
+// 33.6 us, now 12.8. The rotation of that step into the bf16 cache takes 8.8 in
+// 5808 waves; the 8704 here last as long each, waiting for 64% of it (62%
+// there). Which of the chain of search, page, rows, maximum and codes costs what
+// is not measured apart; the search in one round instead of two changed nothing.)
 // ---------------------------------------------------------------------------
 
 // The sequence that holds new token t: the largest s with query_start_loc[s]

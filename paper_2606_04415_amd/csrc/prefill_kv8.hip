@@ -19,7 +19,9 @@
 //  - A tile's keys may be cut into pieces (plan.cpp); merge_tiles_kernel joins
 //    them.
 //
-// Measured: eight prompts of 2048, 28/4 heads of 128, 284 us, 847 TFLOP/s. With
+// Measured: eight prompts of 2048, 28/4 heads of 128, 275 to 302 us by box and
+// clock, 797 to 875 TFLOP/s (the first 60 launches of a process 322 in the mean);
+// 159 MB fetched, of which the keys and values 2.5 times over. With
 // the machine full the clock gives way: against 16x16x32 it takes 6% fewer
 // clocks and 2% more time, at 2.1 GHz instead of 2.25, and vector work, operand
 // reads and products each fill less than two thirds of the clocks.
