@@ -13,8 +13,9 @@
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
+#include <exception>
 #include <functional>
-#include <new>
+#include <memory>
 #include <string>
 
 #include "host_common.h"
@@ -115,9 +116,9 @@ extern "C" const char* flex_attn_status_string(int status) {
 
 extern "C" const char* flex_attn_last_error(void) { return flexattn::last_error(); }
 
-extern "C" int flex_attn_plan(const flex_attn_shape* shape, const flex_attn_plan_opts* opts,
-                              int32_t num_seqs, const int32_t* qsl, const int32_t* seq_lens,
-                              int32_t max_pages_per_seq, flex_attn_plan_t** out_plan) {
+static int plan_batch(const flex_attn_shape* shape, const flex_attn_plan_opts* opts, int32_t num_seqs,
+                      const int32_t* qsl, const int32_t* seq_lens, int32_t max_pages_per_seq,
+                      flex_attn_plan_t** out_plan) {
   clear_error();
   if (!out_plan) return set_error(FLEX_ERR_INVALID_ARG, "out_plan is NULL");
   *out_plan = nullptr;
@@ -556,8 +557,7 @@ extern "C" int flex_attn_plan(const flex_attn_shape* shape, const flex_attn_plan
       for (size_t k = 0; k < lists[x].size(); ++k) fused[8 * k + x] = lists[x][k];
   }
 
-  flex_attn_plan_t* plan = new (std::nothrow) flex_attn_plan_t();
-  if (!plan) return set_error(FLEX_ERR_INTERNAL, "out of host memory");
+  auto plan = std::make_unique<flex_attn_plan_t>();
   plan->shape = sh;
   plan->rows_per_wg = rows_per_wg;
   plan->kv_bits = kv8 ? 8 : 16;
@@ -662,8 +662,19 @@ extern "C" int flex_attn_plan(const flex_attn_shape* shape, const flex_attn_plan
   for (size_t i = size_t(ranges[RA]); i < pieces.size(); ++i)
     info.decode_tail_bytes += double(kv_bytes(pieces[i].k1 - pieces[i].k0));   // (pieces start on a page)
   if (log_level() > 0) log_plan(*plan);
-  *out_plan = plan;
+  *out_plan = plan.release();
   return FLEX_OK;
+}
+
+// The work lists of a long batch may be more than the host has room for.
+extern "C" int flex_attn_plan(const flex_attn_shape* shape, const flex_attn_plan_opts* opts,
+                              int32_t num_seqs, const int32_t* qsl, const int32_t* seq_lens,
+                              int32_t max_pages_per_seq, flex_attn_plan_t** out_plan) {
+  try {
+    return plan_batch(shape, opts, num_seqs, qsl, seq_lens, max_pages_per_seq, out_plan);
+  } catch (const std::exception&) {   // bad_alloc, or length_error
+    return set_error(FLEX_ERR_INTERNAL, "out of memory");   // (short enough to need none)
+  }
 }
 
 extern "C" int flex_attn_validate_host(const flex_attn_plan_t* plan, const int32_t* bt, int32_t bt_stride,

@@ -2,6 +2,7 @@
 refusals of the C calls and of the binding, and plans for 8-bit caches."""
 import ctypes
 import math
+import pathlib
 import random
 
 import numpy as np
@@ -412,6 +413,33 @@ def test_binding_refuses_cpu_tensors_and_other_shapes():
         F.make_kv8_args(t["q"], t["k"], t["v"], t["s"], t["bt"], t["ls"], t["qsl"], t["out"], torch.zeros(3, 27))
     with pytest.raises(ValueError, match="as many sequences"):
         F.make_kv8_args(t["q"], t["k"], t["v"], t["s"], t["bt"], t["ls"], t["qsl"][:2], t["out"])
+
+
+@pytest.mark.parametrize("kv_bits", [8, 16])
+def test_a_plan_that_does_not_fit_the_host_is_an_error(kv_bits):
+    """A prompt whose tiles take gigabytes, in a process that may have a quarter of
+    one more: a status, not an exception through the C call, which would end the
+    process; and the next plan is made."""
+    import subprocess
+    import sys
+    code = f"""
+import resource
+from paper_2606_04415_amd import flexattn as F
+shape = F.make_shape(28, 4, 128, 128, 16, 0.1)
+opts = F.make_opts(kv_bits={kv_bits}, bm=128)
+F.flex_attn_plan(shape, opts, [0, 1], [5], 1)
+held = next(int(x.split()[1]) for x in open("/proc/self/status") if x.startswith("VmSize")) * 1024
+resource.setrlimit(resource.RLIMIT_AS, (held + (256 << 20), resource.RLIM_INFINITY))
+n = 300_000_000
+try:
+    F.flex_attn_plan(shape, opts, [0, n], [n], n // 16)
+    print("made")
+except F.FlexAttnError as e:
+    print("status", e.status, F.flex_attn_plan(shape, opts, [0, 40], [50], 4).info["n_prefill_items"] > 0)
+"""
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=120,
+                       cwd=pathlib.Path(__file__).resolve().parents[1])
+    assert r.stdout.split() == ["status", str(F.FLEX_ERR_INTERNAL), "True"], (r.returncode, r.stdout, r.stderr[-500:])
 
 
 def test_plans_take_the_starts_that_the_batch_needs():
